@@ -228,7 +228,7 @@ def _results(s):
     if c["op"] == "norm":
         out = [s["sum"], s["y"]]
         return out + [s[k] for k in ("mean", "rstd", "dres", "dx", "dgamma", "dbeta")] if c["mode"] == "train" else out
-    return {"serve": [s["out"]], "norm": [s["sum"], s["out"]], "train": [s["out"], s.get("dx"), s.get("dw")]}[c["mode"]]
+    return {"serve": [s["out"]], "norm": [s.get("sum"), s["out"]], "train": [s["out"], s.get("dx"), s.get("dw")]}[c["mode"]]
 
 
 def run(s):
