@@ -447,6 +447,213 @@ typedef struct {
 layup_status layup_gemm_bf16(const layup_gemm_desc* d, void* stream);
 layup_status layup_gemm_f32(const layup_gemm_desc* d, void* stream);
 
+/* ------------------------------------------- dropout, LayerNorm, 8-bit floats
+ *
+ * The way into a linear layer, s = residual + dropout(x), y = LayerNorm(s),
+ * y W^T, as calls of their own beside the raw products, forward and backward.
+ * layup_set_dropout makes the GPT step call the first two.
+ *
+ * Common to them: matrices are row-major, an ld* is the distance of two rows
+ * in elements (>= the row's length).  Pointers are device pointers aligned to
+ * their element (and as stated); larger alignment is only faster.  Elements
+ * behind a row's end and rows behind the last are neither read nor written,
+ * except where stated.  Work runs on `stream` (NULL: the default stream) and
+ * on its device, whatever the current device.  Nothing is allocated and no
+ * state is kept between calls: calls on different streams are independent as
+ * long as their buffers (workspaces included) are, and every call can be
+ * captured into a graph.  Results are the same bit for bit in every run.
+ * Errors through layup_global_error.  Buffers may overlap only as stated. */
+
+typedef enum {
+  LAYUP_F32 = 0,
+  LAYUP_BF16 = 1,
+  LAYUP_E4M3 = 2, /* 8-bit float, 4 exponent bits, largest 448, no infinity (OCP) */
+  LAYUP_E5M2 = 3  /* 8-bit float, 5 exponent bits, largest 57344 (OCP) */
+} layup_dtype;
+
+/* Which elements a dropout keeps: a pure function of (seed, offset, row,
+ * column), so the backward pass and every fused form draw the same mask and
+ * none is stored.  Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011) with key = seed (low word first) and
+ * counter = (column / 8, row, offset low, offset high) gives 128 bits for
+ * eight columns, 16 bits each: column c takes word (c % 8) / 2, its low half
+ * for even c.  The element is kept where these 16 bits are >= T = round(65536
+ * p) (at most 65535) and then multiplied by 65536 / (65536 - T); p counts to
+ * the nearest 1/65536, and the mean is exactly that of x.  A dropped element
+ * is 0 whatever it was.  offset_dev (device uint64, nullable, 8-byte aligned)
+ * is read when the kernel runs and added to offset: a captured graph draws new
+ * masks as the caller advances it.  0 <= p < 1; p below 1/131072 drops nothing. */
+typedef struct {
+  float p;
+  int32_t reserved;
+  uint64_t seed;
+  uint64_t offset;
+  const uint64_t* offset_dev;
+} layup_dropout_mask;
+
+/* y = dropout(x) of a rows x cols matrix, float32 or bfloat16 (computed in
+ * float32, rounded once); its backward is the same call on the gradient.  y
+ * may be x itself (with ldy = ldx).  rows < 2^31, cols < 2^33; rows = 0 or
+ * cols = 0 is a no-op. */
+typedef struct {
+  int64_t rows, cols;
+  const void* x;
+  int64_t ldx;
+  void* y;
+  int64_t ldy;
+  int32_t dtype; /* layup_dtype of x and y */
+  int32_t reserved;
+  layup_dropout_mask drop;
+} layup_dropout_desc;
+layup_status layup_dropout(const layup_dropout_desc* d, void* stream);
+
+/* Forward:  s = residual + dropout(x)   (residual NULL: s = dropout(x)),
+ *           rounded to s_dtype, the type of the residual stream;
+ *           y = (s - mean(s)) / sqrt(var(s) + eps) * gamma + beta  of each row
+ * with the biased variance, everything in float32 (two passes over the row in
+ * registers).  gamma and beta (float32 [d], nullable: 1 and 0).  s is stored
+ * where sum is given (nullable); mean and rstd (float32 [rows], nullable)
+ * receive the row's statistics for the backward.  y_dtype is F32, BF16, or
+ * E4M3 / E5M2: then y holds the 8-bit operand of layup_gemm_fp8 with its
+ * scale bytes in y_scale, as layup_quant_fp8 with block 1 would make of the
+ * float32 y (ldy >= d rounded up to 128, the columns up to there zeroed).
+ * sum may be the residual's own buffer (same ld).  1 <= d <= 16384, rows <
+ * 2^31; rows = 0 is a no-op. */
+typedef struct {
+  int64_t rows;
+  int32_t d;
+  float eps; /* >= 0 */
+  const void* x;
+  int64_t ldx;
+  const void* residual;
+  int64_t ldr;
+  void* sum;
+  int64_t lds;
+  void* y;
+  int64_t ldy;
+  const float* gamma;
+  const float* beta;
+  float* mean;
+  float* rstd;
+  uint8_t* y_scale;
+  int64_t ld_scale;
+  int32_t x_dtype, s_dtype, y_dtype; /* layup_dtype; x, s: F32 or BF16 */
+  int32_t reserved;
+  layup_dropout_mask drop;
+} layup_layernorm_desc;
+layup_status layup_layernorm_forward(const layup_layernorm_desc* d, void* stream);
+
+/* Backward of the above.  With a = dy gamma, xh = (s - mean) rstd:
+ *   ds = dsum + rstd (a - mean(a) - xh mean(a xh))      of each row
+ *   dres = ds (gradient of the residual), dx = dropout(ds) with the forward's
+ *   mask (gradient of x), dgamma = sum over rows of dy xh, dbeta = sum of dy.
+ * s, mean and rstd are the forward's (s: its sum, or x where it had neither
+ * residual nor dropout and s_dtype is x's); dsum (nullable: 0) is the gradient
+ * that reaches s past the LayerNorm.  s, dsum and dres have s_dtype.  dres, dx,
+ * dgamma, dbeta are nullable.  dgamma and dbeta (float32 [d]) are overwritten,
+ * and zeroed for rows = 0; they need workspace
+ * (layup_layernorm_workspace_size bytes, 16-byte aligned).  dres may be dsum's
+ * own buffer (same ld). */
+typedef struct {
+  int64_t rows;
+  int32_t d;
+  int32_t dy_dtype, s_dtype, dx_dtype; /* layup_dtype: F32 or BF16 */
+  const void* dy;
+  int64_t lddy;
+  const void* s;
+  int64_t lds;
+  const void* dsum;
+  int64_t lddsum;
+  const float* mean;
+  const float* rstd;
+  const float* gamma;
+  void* dres;
+  int64_t lddres;
+  void* dx;
+  int64_t lddx;
+  float* dgamma;
+  float* dbeta;
+  void* workspace;
+  size_t workspace_bytes;
+  layup_dropout_mask drop;
+} layup_layernorm_grad_desc;
+layup_status layup_layernorm_backward(const layup_layernorm_grad_desc* d, void* stream);
+layup_status layup_layernorm_workspace_size(int64_t rows, int32_t d, size_t* bytes);
+
+/* A matrix in 8-bit floats with one power-of-two scale for each block of 128
+ * along a row: q(r, c) 2^(scale byte - 127) ~ x(r, c).  block_rows = 1: blocks
+ * of 1 x 128 (activations, gradients); 128: blocks of 128 x 128 (weights).
+ * The scale is the smallest power of two (2^-126 at least) with the block's
+ * largest finite magnitude / scale <= the format's largest value, 1 for a
+ * block of zeros; scaling by it is exact, q is rounded to nearest even.
+ * Infinities and NaN become the format's NaN and do not count for the scale.
+ *   q  (nullable): rows x cols, ldq >= cols rounded up to 128, a multiple of
+ *      16, 16-byte aligned; columns cols .. that end of a row are zeroed.
+ *      Block (r, b) has its byte at scale[(r / block_rows) * ld_scale + b].
+ *   qt (nullable): the transposed matrix, cols x rows, quantised as a matrix of
+ *      its own (its blocks run along x's rows), laid out the same way; with
+ *      block_rows = 128 its values are those of q.
+ * ld_scale (bytes) is a multiple of 4 and at least the number of blocks of a
+ * row, scale 4-byte aligned.  x is float32 or bfloat16.  rows = 0 or cols = 0
+ * is a no-op. */
+typedef struct {
+  int64_t rows, cols;
+  const void* x;
+  int64_t ldx;
+  int32_t x_dtype;    /* LAYUP_F32 or LAYUP_BF16 */
+  int32_t q_dtype;    /* LAYUP_E4M3 or LAYUP_E5M2 */
+  int32_t block_rows; /* 1 or 128 */
+  int32_t reserved;
+  void* q;
+  int64_t ldq;
+  uint8_t* scale;
+  int64_t ld_scale;
+  void* qt;
+  int64_t ldqt;
+  uint8_t* scale_t;
+  int64_t ld_scale_t;
+} layup_quant_desc;
+layup_status layup_quant_fp8(const layup_quant_desc* d, void* stream);
+
+/* C = A B^T (+ bias[n]) of two matrices in 8-bit floats, A: M x K, B: N x K,
+ * both as layup_quant_fp8 leaves them: k-contiguous rows, zeros from K up to a
+ * multiple of 128, scale bytes of blocks of a_block (b_block) rows by 128 k.
+ * float32 accumulation; C float32 or bfloat16 (c_f32 = 0; rounded to nearest
+ * even), any ldc >= N, bias float32 (nullable).  For a bfloat16 C the 8-bit
+ * matrix instructions add groups of eight products dropping what lies 2^-13
+ * below the group's largest (about 1.3e-5 of the result, against 1.7e-3 of the
+ * rounding to bfloat16); for a float32 C the operands are widened exactly and
+ * the sums are float32 sums.  Of a linear layer with weight
+ * W [out, in]: the forward is A = x, B = W; dX is A = dY, B = W^T (quantised
+ * over out); dW is A = dY^T, B = x^T (both quantised over the tokens).  Each
+ * operand is E4M3 or E5M2.  lda, ldb: at least K rounded up to 128, multiples
+ * of 16; A and B 16-byte aligned; scales as layup_quant_fp8 states (bytes 1 to
+ * 254).
+ * workspace (device, optional, 16-byte aligned): float32 split-K partials; K is
+ * split only when they fit, and the summation order, and so the rounding, then
+ * differ.  M = 0 or N = 0 is a no-op; K = 0 writes C = bias (or 0). */
+typedef struct {
+  int64_t M, N, K;
+  const void* A;
+  int64_t lda;
+  const uint8_t* a_scale;
+  int64_t ld_a_scale;
+  const void* B;
+  int64_t ldb;
+  const uint8_t* b_scale;
+  int64_t ld_b_scale;
+  void* C;
+  int64_t ldc;
+  const float* bias;
+  int32_t a_dtype, b_dtype; /* LAYUP_E4M3 or LAYUP_E5M2 */
+  int32_t a_block, b_block; /* 1 or 128: rows that share a scale */
+  int32_t c_f32;
+  int32_t reserved;
+  void* workspace;
+  size_t workspace_bytes;
+} layup_gemm_fp8_desc;
+layup_status layup_gemm_fp8(const layup_gemm_fp8_desc* d, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -265,6 +265,29 @@ hipError_t launch_token_sort(const int32_t* tokens, int B, int T, int V, int32_t
 hipError_t launch_ce_f32(const float* logits, const int32_t* labels, int rows, int V,
                          float* dlogits, float* loss_rows, float* loss_out, hipStream_t s);
 
+// ------------------------------------------- dropout, LayerNorm, 8-bit floats
+// What a kernel needs of a layup_dropout_mask: key, the threshold the 16 bits
+// are held against in the high half of a word, the factor of kept elements.
+struct Mask {
+  uint32_t k0, k1;
+  uint32_t thr;  // T << 16; 0: no dropout
+  float scale;
+  uint64_t offset;
+  const uint64_t* offset_dev;
+};
+Mask make_mask(const layup_dropout_mask& d);
+hipError_t launch_dropout(const layup_dropout_desc& d, const Mask& k, hipStream_t s);
+constexpr int NORM_MAX_D = 16384;
+hipError_t launch_norm_fwd(const layup_layernorm_desc& d, const Mask& k, hipStream_t s);
+// dgamma, dbeta: with part (norm_partial_floats floats) and then a second launch
+hipError_t launch_norm_bwd(const layup_layernorm_grad_desc& d, const Mask& k, hipStream_t s);
+int64_t norm_partial_floats(int64_t rows, int d);
+hipError_t launch_quant_fp8(const layup_quant_desc& d, hipStream_t s);
+hipError_t launch_gemm_fp8(const layup_gemm_fp8_desc& d, hipStream_t s);
+
+// Records the text of a context-free call's error; returns st.  (model.hip)
+layup_status global_fail(layup_status st, const std::string& msg);
+
 }  // namespace layup
 
 // ------------------------------------------------------------ test entries

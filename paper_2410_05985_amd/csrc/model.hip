@@ -146,6 +146,11 @@ bool fused_attention(const layup_config& g) {
 
 }  // namespace
 
+layup_status layup::global_fail(layup_status st, const std::string& msg) {
+  g_err = msg;
+  return st;
+}
+
 struct layup_ctx {
   layup_config cfg;
   Layout L;

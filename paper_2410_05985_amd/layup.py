@@ -22,6 +22,7 @@ LAYUP_SGD_MOMENTUM, LAYUP_ADAMW = 0, 1
 LAYUP_MODEL_MLP_F32, LAYUP_MODEL_GPT_BF16 = 0, 1
 LAYUP_MAX_MLP_LAYERS = 8
 LAYUP_MIX_PULL, LAYUP_MIX_PUSH = 0, 1
+LAYUP_F32, LAYUP_BF16, LAYUP_E4M3, LAYUP_E5M2 = 0, 1, 2, 3
 LAYUP_SCHEDULE_LAYERWISE, LAYUP_SCHEDULE_AFTER_BACKWARD, LAYUP_SCHEDULE_FUSED_DW = 0, 1, 2
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "SHAPE", 3: "ALIGN", 4: "DTYPE", 5: "STATE", 6: "HIP"}
@@ -81,6 +82,51 @@ class layup_gemm_desc(C.Structure):
                 ("a_rowsum", C.c_void_p)]
 
 
+class layup_dropout_mask(C.Structure):
+    _fields_ = [("p", C.c_float), ("reserved", C.c_int32), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("offset_dev", C.c_void_p)]
+
+
+class layup_dropout_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("y", C.c_void_p), ("ldy", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32),
+                ("drop", layup_dropout_mask)]
+
+
+class layup_layernorm_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int32), ("eps", C.c_float), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("residual", C.c_void_p), ("ldr", C.c_int64), ("sum", C.c_void_p), ("lds", C.c_int64),
+                ("y", C.c_void_p), ("ldy", C.c_int64), ("gamma", C.c_void_p), ("beta", C.c_void_p),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p), ("y_scale", C.c_void_p), ("ld_scale", C.c_int64),
+                ("x_dtype", C.c_int32), ("s_dtype", C.c_int32), ("y_dtype", C.c_int32), ("reserved", C.c_int32),
+                ("drop", layup_dropout_mask)]
+
+
+class layup_layernorm_grad_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int32), ("dy_dtype", C.c_int32), ("s_dtype", C.c_int32),
+                ("dx_dtype", C.c_int32), ("dy", C.c_void_p), ("lddy", C.c_int64), ("s", C.c_void_p),
+                ("lds", C.c_int64), ("dsum", C.c_void_p), ("lddsum", C.c_int64), ("mean", C.c_void_p),
+                ("rstd", C.c_void_p), ("gamma", C.c_void_p), ("dres", C.c_void_p), ("lddres", C.c_int64),
+                ("dx", C.c_void_p), ("lddx", C.c_int64), ("dgamma", C.c_void_p), ("dbeta", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("drop", layup_dropout_mask)]
+
+
+class layup_quant_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("x_dtype", C.c_int32), ("q_dtype", C.c_int32), ("block_rows", C.c_int32), ("reserved", C.c_int32),
+                ("q", C.c_void_p), ("ldq", C.c_int64), ("scale", C.c_void_p), ("ld_scale", C.c_int64),
+                ("qt", C.c_void_p), ("ldqt", C.c_int64), ("scale_t", C.c_void_p), ("ld_scale_t", C.c_int64)]
+
+
+class layup_gemm_fp8_desc(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("A", C.c_void_p), ("lda", C.c_int64),
+                ("a_scale", C.c_void_p), ("ld_a_scale", C.c_int64), ("B", C.c_void_p), ("ldb", C.c_int64),
+                ("b_scale", C.c_void_p), ("ld_b_scale", C.c_int64), ("C", C.c_void_p), ("ldc", C.c_int64),
+                ("bias", C.c_void_p), ("a_dtype", C.c_int32), ("b_dtype", C.c_int32), ("a_block", C.c_int32),
+                ("b_block", C.c_int32), ("c_f32", C.c_int32), ("reserved", C.c_int32), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
 # exported names, in header order
 EXPORTS = [
     "layup_param_layout", "layup_tensor_layout", "layup_workspace_size", "layup_init",
@@ -90,6 +136,8 @@ EXPORTS = [
     "layup_unit_update_push", "layup_step_ex", "layup_step",
     "layup_unit_timeline", "layup_gemm_timing", "layup_gemm_timing_read", "layup_push_sum_send", "layup_push_sum_receive", "layup_activation",
     "layup_gemm_bf16", "layup_gemm_f32",
+    "layup_dropout", "layup_layernorm_forward", "layup_layernorm_backward", "layup_layernorm_workspace_size",
+    "layup_quant_fp8", "layup_gemm_fp8",
 ]
 
 _lib: Optional[C.CDLL] = None
@@ -133,6 +181,12 @@ def lib() -> C.CDLL:
         "layup_activation": ([P, C.c_int32, C.c_int32, P, P, P], C.c_int),
         "layup_gemm_bf16": ([P, P], C.c_int),
         "layup_gemm_f32": ([P, P], C.c_int),
+        "layup_dropout": ([P, P], C.c_int),
+        "layup_layernorm_forward": ([P, P], C.c_int),
+        "layup_layernorm_backward": ([P, P], C.c_int),
+        "layup_layernorm_workspace_size": ([C.c_int64, C.c_int32, P], C.c_int),
+        "layup_quant_fp8": ([P, P], C.c_int),
+        "layup_gemm_fp8": ([P, P], C.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -364,6 +418,189 @@ def layup_gemm_bf16(desc: layup_gemm_desc, stream=None):
 
 def layup_gemm_f32(desc: layup_gemm_desc, stream=None):
     _check(lib().layup_gemm_f32(C.byref(desc), _stream(stream)))
+
+
+# ------------------------------------- dropout, LayerNorm, 8-bit floats
+# The descriptors take torch tensors and read sizes, row distances and types
+# from them (the elements of a row are adjacent) and keep them alive (`kept`).
+
+
+def _dtype(t) -> int:
+    name = str(t.dtype)
+    codes = {"torch.float32": LAYUP_F32, "torch.bfloat16": LAYUP_BF16, "torch.float8_e4m3fn": LAYUP_E4M3,
+             "torch.float8_e5m2": LAYUP_E5M2}
+    if name not in codes:
+        raise TypeError(f"no layup_dtype for {name}")
+    return codes[name]
+
+
+def _matrix(t, shape=None):
+    """(address, row distance) of a 2-d tensor; of None: (None, 0)."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("a matrix with adjacent elements in a row is needed")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"matrix of {tuple(t.shape)} where {tuple(shape)} is needed")
+    # a single row may come with any stride: rows are at least their length apart
+    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _vector(t, n: int, kind: str):
+    if t is None:
+        return None
+    if str(t.dtype) != kind or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{n} adjacent values of {kind} are needed")
+    return t.data_ptr()
+
+
+def _same_type(*ts):
+    codes = {_dtype(t) for t in ts if t is not None}
+    if len(codes) > 1:
+        raise TypeError("these tensors share one type")
+    return codes.pop() if codes else None
+
+
+def _mask(p, seed, offset, offset_dev) -> layup_dropout_mask:
+    if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+        raise ValueError("seed and offset are unsigned 64-bit numbers")
+    return layup_dropout_mask(p=p, seed=seed, offset=offset, offset_dev=_ptr(offset_dev))
+
+
+def dropout_desc(x, y, p: float, seed: int = 0, offset: int = 0, offset_dev=None) -> layup_dropout_desc:
+    d = layup_dropout_desc()
+    d.rows, d.cols = x.shape
+    d.x, d.ldx = _matrix(x)
+    d.y, d.ldy = _matrix(y, x.shape)
+    d.dtype = _same_type(x, y)
+    d.drop = _mask(p, seed, offset, offset_dev)
+    d.kept = (x, y, offset_dev)
+    return d
+
+
+def layup_dropout(desc: layup_dropout_desc, stream=None):
+    _check(lib().layup_dropout(C.byref(desc), _stream(stream)))
+
+
+def layernorm_desc(x, y, gamma=None, beta=None, residual=None, sum_out=None, mean=None, rstd=None, eps: float = 1e-5,
+                   y_scale=None, s_dtype: Optional[int] = None, p: float = 0.0, seed: int = 0, offset: int = 0,
+                   offset_dev=None) -> layup_layernorm_desc:
+    """y may be an 8-bit matrix, as wide as d rounded up to 128, with y_scale.  s_dtype: the type of the sum where
+    neither residual nor sum_out says it (default: x's)."""
+    d = layup_layernorm_desc()
+    d.rows, d.d = x.shape
+    d.eps = eps
+    d.x, d.ldx = _matrix(x)
+    d.residual, d.ldr = _matrix(residual, x.shape)
+    d.sum, d.lds = _matrix(sum_out, x.shape)
+    d.x_dtype, d.y_dtype = _dtype(x), _dtype(y)
+    st = _same_type(residual, sum_out)
+    d.s_dtype = st if st is not None else d.x_dtype if s_dtype is None else s_dtype
+    eight = d.y_dtype in (LAYUP_E4M3, LAYUP_E5M2)
+    d.y, d.ldy = _matrix(y, None if eight else x.shape)
+    if eight:
+        _eight(y, *x.shape)
+        d.y_scale, d.ld_scale = _scale(y_scale, x.shape[0], x.shape[1])
+    d.gamma, d.beta = (_vector(v, d.d, "torch.float32") for v in (gamma, beta))
+    d.mean, d.rstd = (_vector(v, d.rows, "torch.float32") for v in (mean, rstd))
+    d.drop = _mask(p, seed, offset, offset_dev)
+    d.kept = (x, y, gamma, beta, residual, sum_out, mean, rstd, y_scale, offset_dev)
+    return d
+
+
+def layup_layernorm_forward(desc: layup_layernorm_desc, stream=None):
+    _check(lib().layup_layernorm_forward(C.byref(desc), _stream(stream)))
+
+
+def layup_layernorm_workspace_size(rows: int, d: int) -> int:
+    n = C.c_size_t()
+    _check(lib().layup_layernorm_workspace_size(rows, d, C.byref(n)))
+    return n.value
+
+
+def layernorm_grad_desc(dy, s, mean, rstd, gamma=None, dsum=None, dres=None, dx=None, dgamma=None, dbeta=None,
+                        workspace=None, p: float = 0.0, seed: int = 0, offset: int = 0,
+                        offset_dev=None) -> layup_layernorm_grad_desc:
+    d = layup_layernorm_grad_desc()
+    d.rows, d.d = dy.shape
+    d.dy, d.lddy = _matrix(dy)
+    d.s, d.lds = _matrix(s, dy.shape)
+    d.dsum, d.lddsum = _matrix(dsum, dy.shape)
+    d.dres, d.lddres = _matrix(dres, dy.shape)
+    d.dx, d.lddx = _matrix(dx, dy.shape)
+    d.dy_dtype, d.s_dtype = _dtype(dy), _same_type(s, dsum, dres)
+    d.dx_dtype = d.dy_dtype if dx is None else _dtype(dx)
+    d.gamma, d.dgamma, d.dbeta = (_vector(v, d.d, "torch.float32") for v in (gamma, dgamma, dbeta))
+    d.mean, d.rstd = (_vector(v, d.rows, "torch.float32") for v in (mean, rstd))
+    if workspace is not None:
+        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    d.drop = _mask(p, seed, offset, offset_dev)
+    d.kept = (dy, s, mean, rstd, gamma, dsum, dres, dx, dgamma, dbeta, workspace, offset_dev)
+    return d
+
+
+def layup_layernorm_backward(desc: layup_layernorm_grad_desc, stream=None):
+    _check(lib().layup_layernorm_backward(C.byref(desc), _stream(stream)))
+
+
+def _eight(q, rows: int, k: int):
+    """(address, row distance) of an 8-bit matrix of `rows` rows, each k elements and the zeros up to a multiple of 128."""
+    if _dtype(q) not in (LAYUP_E4M3, LAYUP_E5M2):
+        raise TypeError("an 8-bit matrix is needed")
+    if q.dim() != 2 or q.shape[0] != rows or q.shape[1] < (k + 127) // 128 * 128:
+        raise ValueError(f"an 8-bit matrix of {rows} rows of {k} elements, rounded up to 128, is needed")
+    return _matrix(q)
+
+
+def _scale(t, rows: int, k: int):
+    """(address, row distance) of the scale bytes of `rows` rows of blocks."""
+    if t is None or str(t.dtype) != "torch.uint8" or t.dim() != 2 or t.shape[0] < rows or t.shape[1] < (k + 127) // 128:
+        raise ValueError(f"a table of {rows} rows of {(k + 127) // 128} scale bytes is needed")
+    return _matrix(t)
+
+
+def quant_desc(x, block_rows: int, q=None, scale=None, qt=None, scale_t=None) -> layup_quant_desc:
+    d = layup_quant_desc()
+    d.rows, d.cols = rows, cols = x.shape
+    d.x, d.ldx = _matrix(x)
+    d.x_dtype, d.block_rows = _dtype(x), block_rows
+    if q is not None or qt is not None:
+        d.q_dtype = _same_type(q, qt)
+    if q is not None:
+        d.q, d.ldq = _eight(q, rows, cols)
+        d.scale, d.ld_scale = _scale(scale, -(-rows // max(1, block_rows)), cols)
+    if qt is not None:
+        d.qt, d.ldqt = _eight(qt, cols, rows)
+        d.scale_t, d.ld_scale_t = _scale(scale_t, -(-cols // max(1, block_rows)), rows)
+    d.kept = (x, q, scale, qt, scale_t)
+    return d
+
+
+def layup_quant_fp8(desc: layup_quant_desc, stream=None):
+    _check(lib().layup_quant_fp8(C.byref(desc), _stream(stream)))
+
+
+def gemm_fp8_desc(A, a_scale, a_block: int, B, b_scale, b_block: int, C_, K: int, bias=None,
+                  workspace=None) -> layup_gemm_fp8_desc:
+    """C_ [M, N] = A [M, K] B [N, K]^T; A and B as layup_quant_fp8 leaves them, a_block and b_block its block_rows."""
+    d = layup_gemm_fp8_desc()
+    d.M, d.N, d.K = C_.shape[0], C_.shape[1], K
+    d.C, d.ldc = _matrix(C_)
+    d.c_f32 = {LAYUP_F32: 1, LAYUP_BF16: 0}[_dtype(C_)]
+    d.A, d.lda = _eight(A, d.M, K)
+    d.B, d.ldb = _eight(B, d.N, K)
+    d.a_scale, d.ld_a_scale = _scale(a_scale, -(-d.M // max(1, a_block)), K)
+    d.b_scale, d.ld_b_scale = _scale(b_scale, -(-d.N // max(1, b_block)), K)
+    d.a_dtype, d.b_dtype, d.a_block, d.b_block = _dtype(A), _dtype(B), a_block, b_block
+    d.bias = _vector(bias, d.N, "torch.float32")
+    if workspace is not None:
+        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    d.kept = (A, a_scale, B, b_scale, C_, bias, workspace)
+    return d
+
+
+def layup_gemm_fp8(desc: layup_gemm_fp8_desc, stream=None):
+    _check(lib().layup_gemm_fp8(C.byref(desc), _stream(stream)))
 
 
 # ------------------------------------------------------------- harness

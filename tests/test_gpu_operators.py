@@ -1,0 +1,596 @@
+"""Dropout, LayerNorm with its residual add, and matrices in 8-bit floats against the float64 reference
+(oracle/operators_ref.py), through the C ABI.
+
+Tolerances count roundings.  u = 2^-24 is half a step of float32, EPS[t] half a step of an output type.  A float32 sum
+of at most n terms in a row, then a tree, is off by at most (n + 30) u of the sum of absolute values; a thread of the
+LayerNorm kernels adds at most 32 terms of a row before the tree, so 64 u covers a row's sum and its scaling."""
+import numpy as np
+import pytest
+
+from oracle import operators_ref as R
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+from paper_2410_05985_amd import layup as LU  # noqa: E402
+
+DEV = "cuda"
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24
+EPS = {F32: U, BF16: 2.0 ** -8}
+FP8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64) if t.dtype != torch.float64 else t.cpu().numpy()
+
+
+def matrix(rng, rows, cols, dtype, pad=0, scale=1.0, shift=0.0, fill=7.0):
+    """A matrix inside a larger buffer whose other elements are `fill`; rows cols + pad apart, two rows behind."""
+    m = torch.full((rows + 2, cols + pad), fill, dtype=F32)
+    m[:rows, :cols] = torch.from_numpy(rng.normal(size=(rows, cols)) * scale + shift).float()
+    return m.to(dtype).to(DEV)[:rows, :cols]
+
+
+def whole(t):
+    """The buffer that a `matrix` lies in."""
+    return t._base if t._base is not None else t
+
+
+def untouched(t, fill=7.0):
+    b = whole(t).float().cpu()
+    b = b.reshape(-1, t.stride(0)) if b.dim() == 1 else b
+    inside = torch.zeros_like(b, dtype=torch.bool)
+    inside[: t.shape[0], : t.shape[1]] = True
+    assert bool((b[~inside] == fill).all()), "elements outside the matrix were written"
+
+
+def near(got, ref, tol, what):
+    got, ref = np.asarray(got, np.float64), np.asarray(ref, np.float64)
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    bad = ~(np.abs(got - ref) <= tol)
+    if bad.any():
+        i = np.unravel_index(np.argmax(np.where(bad, np.abs(got - ref) / np.maximum(tol, 1e-300), 0)), bad.shape)
+        tol = np.broadcast_to(tol, bad.shape)
+        raise AssertionError(f"{what}: {bad.sum()} of {bad.size} off; at {i}: {got[i]!r} against {ref[i]!r}, allowed {tol[i]:.3e}")
+
+
+# ---------------------------------------------------------------- dropout
+
+
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 7, 0), (3, 8, 0), (5, 9, 2), (33, 516, 4), (1003, 129, 1), (2, 70000, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.99])
+def test_dropout_is_the_masks(rows, cols, pad, dtype, p):
+    """Bit for bit: one float32 product, one rounding to the type."""
+    rng = np.random.default_rng(rows + cols)
+    x = matrix(rng, rows, cols, dtype, pad)
+    y = matrix(rng, rows, cols, dtype, pad + 3)
+    seed, offset = 0xFEDCBA9876543210, (1 << 63) + 5
+    LU.layup_dropout(LU.dropout_desc(x, y, p=p, seed=seed, offset=offset), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    keep = torch.from_numpy(R.keep_mask(rows, cols, p, seed, offset)) if R.drop_threshold(p) else torch.ones(rows, cols, dtype=torch.bool)
+    ref = torch.where(keep, x.float().cpu() * np.float32(R.drop_scale(p)), torch.zeros(())).to(dtype)
+    assert torch.equal(y.cpu(), ref)
+    untouched(y)
+    LU.layup_dropout(LU.dropout_desc(x, x, p=p, seed=seed, offset=offset))  # in place, on the default stream
+    torch.cuda.synchronize()
+    assert torch.equal(x.cpu(), ref)
+    untouched(x)
+
+
+def test_dropout_of_what_is_not_finite():
+    x = torch.full((4, 64), float("inf"), device=DEV)
+    x[1] = float("nan")
+    LU.layup_dropout(LU.dropout_desc(x, x, p=0.5, seed=1))
+    torch.cuda.synchronize()
+    keep = torch.from_numpy(R.keep_mask(4, 64, 0.5, 1, 0))
+    x = x.cpu()
+    assert bool((x[~keep] == 0).all()) and not bool(torch.isfinite(x[keep]).any())
+
+
+def test_dropout_offset_from_the_device_in_a_graph():
+    """A captured call draws the masks of the counter it finds at each replay."""
+    x = torch.ones(40, 100, device=DEV)
+    y = torch.empty_like(x)
+    counter = torch.zeros(1, dtype=torch.int64, device=DEV)
+    s = torch.cuda.Stream()
+    desc = LU.dropout_desc(x, y, p=0.3, seed=5, offset=(1 << 64) - 1, offset_dev=counter)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        LU.layup_dropout(desc, s)
+        s.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            LU.layup_dropout(desc, torch.cuda.current_stream())
+            counter.add_(3)
+    counter.zero_()
+    torch.cuda.synchronize()
+    for k in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = R.dropout(np.ones((40, 100)), 0.3, 5, (1 << 64) - 1 + 3 * k)
+        near(f64(y), ref, 2 * U * ref, f"replay {k}")
+
+
+# -------------------------------------------------------------- LayerNorm
+
+WIDTHS = [1, 7, 8, 9, 127, 256, 257, 520, 768, 1000, 1024, 1025, 1237, 2048, 2049, 4096, 4100, 8192, 8193, 16383, 16384]
+
+
+def forward(rng, rows, d, tx, ts, ty, p, pad, residual=True, affine=True, eps=1e-5, seed=11, offset=(1 << 32) + 1):
+    x = matrix(rng, rows, d, tx, pad)
+    r = matrix(rng, rows, d, ts, pad + 1, 2.0, 0.5) if residual else None
+    s, y = matrix(rng, rows, d, ts, pad + 2), matrix(rng, rows, d, ty, pad)
+    g = torch.from_numpy(rng.normal(size=d)).float().to(DEV) if affine else None
+    b = torch.from_numpy(rng.normal(size=d)).float().to(DEV) if affine else None
+    mean, rstd = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, y, g, b, residual=r, sum_out=s, mean=mean, rstd=rstd, eps=eps, p=p,
+                                                 seed=seed, offset=offset), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    exact_s = R.dropout(f64(x), p, seed, offset) + (f64(r) if residual else 0.0)
+    # product and sum in float32, then the stream's type; nearest rounding of a
+    # value that is itself off by err is off by err more
+    err = 2 * U * (np.abs(R.dropout(f64(x), p, seed, offset)) + np.abs(exact_s))
+    near(f64(s), exact_s, err + EPS[ts] * (np.abs(exact_s) + err), "sum")
+    sv = f64(s)
+    ref, m, q = R.norm_fwd(sv, f64(g) if affine else 1.0, f64(b) if affine else 0.0, eps)
+    dm = 64 * U * np.abs(sv).mean(1)
+    near(f64(mean), m, dm, "mean")
+    # the mean's error counts once in every deviation and squared in the variance
+    var = ((sv - m[:, None]) ** 2).mean(1)
+    rel = 40 * U + dm ** 2 / (var + eps)
+    near(f64(rstd), q, rel * q, "rstd")
+    ga, ba = (np.abs(f64(g)), np.abs(f64(b))) if affine else (1.0, 0.0)
+    dev = np.abs(sv - m[:, None]) * q[:, None] * ga
+    tol = dev * (rel + 4 * U)[:, None] + (dm * q)[:, None] * ga * 1.01 + 2 * U * (dev + ba)
+    near(f64(y), ref, tol + EPS[ty] * (np.abs(ref) + tol), "y")
+    for t in (s, y):
+        untouched(t)
+    return x, r, s, y, g, b, mean, rstd
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("tx,ts,ty", [(BF16, F32, BF16), (F32, BF16, F32), (BF16, BF16, BF16), (F32, F32, F32)])
+def test_norm_forward(d, tx, ts, ty):
+    rng = np.random.default_rng(d)
+    forward(rng, 5 if d > 4096 else 19, d, tx, ts, ty, p=0.2, pad=d % 3)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 8, 9, 1003])
+@pytest.mark.parametrize("kw", [dict(residual=False, p=0.0), dict(residual=False, p=0.4), dict(affine=False, p=0.0)])
+def test_norm_forward_without_parts(rows, kw):
+    forward(np.random.default_rng(rows), rows, 264, BF16, F32, BF16, pad=0, **kw)
+
+
+def test_norm_statistics_are_optional_and_sum_in_place():
+    rng = np.random.default_rng(8)
+    x, r, s, y, g, b, _, _ = forward(rng, 37, 776, BF16, BF16, BF16, p=0.1, pad=0)
+    y2 = torch.zeros_like(y)
+    kw = dict(p=0.1, seed=11, offset=(1 << 32) + 1)
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, y2, g, b, residual=r, **kw))
+    torch.cuda.synchronize()
+    assert torch.equal(y, y2)
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, y2, g, b, residual=r, sum_out=r, **kw))
+    torch.cuda.synchronize()
+    assert torch.equal(y, y2) and torch.equal(r, s)
+
+
+def test_norm_rows_that_are_constant_huge_or_not_finite():
+    """A constant row normalises to beta exactly where its mean is exact; NaN and infinities stay in their row."""
+    d = 768
+    x = torch.randn(8, d, device=DEV)
+    x[0], x[1], x[2] = 0.0, 4.0, float("nan")
+    x[3, 5] = float("inf")
+    x[4] *= 1e15
+    y = torch.empty_like(x)
+    b = torch.randn(d, device=DEV)
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, y, None, b))
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], b) and torch.equal(y[1], b)
+    assert bool(torch.isnan(y[2]).all()) and bool(torch.isnan(y[3]).all())
+    assert bool(torch.isfinite(y[4:]).all())
+
+
+def backward_ref(dy, s, mean, rstd, g, dsum, p, seed, offset):
+    """(ds, dx, dgamma, dbeta) and how far each may be off before it is rounded to its type."""
+    ds, dg, db = R.norm_bwd(dy, s, mean, rstd, g, dsum)
+    xh = (s - mean[:, None]) * rstd[:, None]
+    a = dy * g
+    m1, m2 = np.abs(a).mean(1, keepdims=True), np.abs(a * xh).mean(1, keepdims=True)
+    inner = np.abs(a) + m1 + np.abs(xh) * m2
+    tol = 80 * U * rstd[:, None] * inner + 2 * U * (np.abs(dsum) + np.abs(ds))
+    keep = np.where(R.keep_mask(*dy.shape, p, seed, offset), R.drop_scale(p), 0.0) if R.drop_threshold(p) else 1.0
+    n = dy.shape[0]
+    # a thread's rows one after another, at most all of them
+    tg = (min(n, 200) + 80) * U
+    return (ds, tol), (ds * keep, keep * (tol + U * np.abs(ds))), (dg, tg * np.abs(dy * xh).sum(0)), (db, tg * np.abs(dy).sum(0))
+
+
+def backward(rng, rows, d, ty, ts, tx, p, pad, dsum=True, affine=True, inplace=False, want=("dres", "dx", "dgamma", "dbeta")):
+    dy, s = matrix(rng, rows, d, ty, pad), matrix(rng, rows, d, ts, pad + 1, 2.0, 0.5)
+    ds_in = matrix(rng, rows, d, ts, pad) if dsum else None
+    g = torch.from_numpy(rng.normal(size=d)).float().to(DEV) if affine else None
+    _, m, q = R.norm_fwd(f64(s), 1.0, 0.0, 1e-5)
+    mean, rstd = (torch.from_numpy(v).float().to(DEV) for v in (m, q))
+    din = f64(ds_in) if dsum else 0.0 * f64(s)
+    out = dict(dres=ds_in if inplace else matrix(rng, rows, d, ts, pad + 2), dx=matrix(rng, rows, d, tx, pad + 1),
+               dgamma=torch.full((d,), 9.0, device=DEV), dbeta=torch.full((d,), 9.0, device=DEV))
+    out = {k: v for k, v in out.items() if k in want}
+    seed, offset = 99, 1 << 33
+    ws = torch.full((LU.layup_layernorm_workspace_size(rows, d) // 4,), float("nan"), device=DEV)
+    LU.layup_layernorm_backward(LU.layernorm_grad_desc(dy, s, mean, rstd, g, dsum=ds_in, workspace=ws, p=p, seed=seed, offset=offset, **out),
+                                torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    refs = backward_ref(f64(dy), f64(s), f64(mean), f64(rstd), f64(g) if affine else 1.0, din, p, seed, offset)
+    for name, (ref, tol) in zip(("dres", "dx", "dgamma", "dbeta"), refs):
+        if name in out:
+            near(f64(out[name]), ref, tol + EPS[out[name].dtype] * (np.abs(ref) + tol), name)
+            if out[name].dim() == 2:
+                untouched(out[name])
+    return out
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("ty,ts,tx", [(F32, F32, BF16), (BF16, F32, BF16), (F32, BF16, F32), (BF16, BF16, BF16)])
+def test_norm_backward(d, ty, ts, tx):
+    backward(np.random.default_rng(d), 5 if d > 4096 else 19, d, ty, ts, tx, p=0.2, pad=d % 3)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 7, 8, 9, 511, 4097])
+def test_norm_backward_rows(rows):
+    backward(np.random.default_rng(rows), rows, 136, BF16, F32, BF16, p=0.1, pad=0)
+
+
+@pytest.mark.parametrize("rows,d", [(1030, 1024), (600, 2048), (530, 4096), (515, 8200)])
+def test_norm_backward_more_rows_than_blocks(rows, d):
+    backward(np.random.default_rng(d), rows, d, BF16, BF16, BF16, p=0.0, pad=0)
+
+
+@pytest.mark.parametrize("kw", [dict(dsum=False), dict(affine=False), dict(inplace=True), dict(want=("dgamma", "dbeta")),
+                                dict(want=("dx",)), dict(want=("dres",)), dict(want=("dbeta",)), dict(want=("dgamma", "dx"))])
+def test_norm_backward_without_parts(kw):
+    backward(np.random.default_rng(4), 45, 392, F32, F32, BF16, p=0.3, pad=0, **kw)
+
+
+def test_norm_backward_of_no_rows_zeroes_the_weights():
+    z = torch.zeros(0, 24, device=DEV)
+    one = torch.zeros(0, device=DEV)
+    dg, db = torch.ones(24, device=DEV), torch.ones(24, device=DEV)
+    LU.layup_layernorm_backward(LU.layernorm_grad_desc(z, z, one, one, dgamma=dg, dbeta=db))
+    torch.cuda.synchronize()
+    assert not bool(dg.any()) and not bool(db.any())
+
+
+def test_norm_backward_is_the_same_every_time():
+    a, b = (backward(np.random.default_rng(1), 3000, 768, BF16, F32, BF16, p=0.1, pad=0) for _ in range(2))
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+
+
+def test_norm_gradient_by_differences():
+    """The gradient of sum(w y) and of the residual path against central differences of the library's own forward, in
+    float32: a step h changes the sum of n terms of size t by about h; its rounding is u t n / h, the third derivative
+    h^2 (here below 1, with deviations of the rows around 1)."""
+    rng = np.random.default_rng(2)
+    rows, d, h, seed = 3, 24, 2.0 ** -6, 4
+    x, r, w = (torch.from_numpy(rng.normal(size=(rows, d))).float().to(DEV) for _ in range(3))
+    g, b = (torch.from_numpy(rng.normal(size=d)).float().to(DEV) for _ in range(2))
+    kw = dict(p=0.25, seed=seed)
+
+    def f(x, r, g, b):
+        y, s, m, q = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        LU.layup_layernorm_forward(LU.layernorm_desc(x, y, g, b, residual=r, sum_out=s, mean=m, rstd=q, **kw))
+        torch.cuda.synchronize()
+        return (f64(y) * f64(w)).sum(), s, m, q
+
+    _, s, m, q = f(x, r, g, b)
+    dres, dx, dg, db = torch.empty_like(x), torch.empty_like(x), torch.empty_like(g), torch.empty_like(g)
+    ws = torch.empty(LU.layup_layernorm_workspace_size(rows, d), dtype=torch.uint8, device=DEV)
+    LU.layup_layernorm_backward(LU.layernorm_grad_desc(w, s, m, q, g, dres=dres, dx=dx, dgamma=dg, dbeta=db, workspace=ws, **kw))
+    torch.cuda.synchronize()
+    args = dict(x=x, r=r, g=g, b=b)
+    for name, grad in (("x", dx), ("r", dres), ("g", dg), ("b", db)):
+        for i in list(np.ndindex(*args[name].shape))[::7]:
+            up, down = args[name].clone(), args[name].clone()
+            up[i] += h
+            down[i] -= h
+            diff = (f(**{**args, name: up})[0] - f(**{**args, name: down})[0]) / (2 * h)
+            assert abs(diff - grad[i].item()) <= 10 * h * h + 100 * U * rows * d / h, (name, i)
+
+
+# ------------------------------------------------------------ 8-bit floats
+
+
+def room8(rows, k, fmt):
+    """An 8-bit matrix with one more 16 bytes a row and a row behind, all bytes 0x55; its scale table likewise."""
+    kp = -(-k // 128) * 128
+    q = torch.full((rows + 1, kp + 16), 0x55, dtype=torch.uint8, device=DEV)
+    return q.view(FP8[fmt])[:rows]
+
+
+def scale_room(rows, k):
+    return torch.full((rows + 1, -(-(-(-k // 128)) // 4) * 4 + 4), 0x55, dtype=torch.uint8, device=DEV)[:rows]
+
+
+def check_quant(q, e, x, fmt, block_rows, what):
+    ref, eref = R.quantise(x, fmt, block_rows)
+    rows, k = x.shape
+    kp = -(-k // 128) * 128
+    raw = whole(q).view(torch.uint8).cpu() if whole(q).dtype != torch.uint8 else whole(q).cpu()
+    raw = raw.reshape(rows + 1, kp + 16)
+    assert bool((raw[:rows, k:kp] == 0).all()), what + ": padding"
+    assert bool((raw[:rows, kp:] == 0x55).all()) and bool((raw[rows:] == 0x55).all()), what + ": bytes outside"
+    es = whole(e).cpu()
+    nr, nb = eref.shape
+    assert np.array_equal(es[:nr, :nb].numpy(), eref), what + ": scales"
+    assert bool((es[:nr, nb:] == 0x55).all()) and bool((es[nr:] == 0x55).all()), what + ": scale bytes outside"
+    got = raw[:rows, :k].contiguous().view(FP8[fmt]).double().numpy()
+    assert np.array_equal(got, ref, equal_nan=True), what + ": values"
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 2048), (5, 127), (127, 5), (128, 128), (129, 257), (300, 136), (33, 1000)])
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_quantise_both_ways(rows, cols, block_rows, fmt, dtype):
+    """Every byte: values, scales, the zeros behind a row; nothing else is written."""
+    rng = np.random.default_rng(rows * 7 + cols)
+    x = matrix(rng, rows, cols, dtype, 3)
+    x *= torch.exp(5 * torch.randn(rows, 1, device=DEV)).to(dtype)  # scales far apart
+    if rows > 4:
+        x[1] = 0
+        x[2, :3] = torch.tensor([float("inf"), float("-inf"), float("nan")], dtype=dtype)
+        x[3] = 1e-40  # subnormal: the least scale
+        x[4, 0] = 1.75 * 2.0 ** 100  # exactly the largest value
+    q, qt = room8(rows, cols, fmt), room8(cols, rows, fmt)
+    e, et = scale_room(-(-rows // block_rows), cols), scale_room(-(-cols // block_rows), rows)
+    s = torch.cuda.current_stream()
+    LU.layup_quant_fp8(LU.quant_desc(x, block_rows, q=q, scale=e, qt=qt, scale_t=et), s)
+    torch.cuda.synchronize()
+    check_quant(q, e, f64(x), fmt, block_rows, "q")
+    check_quant(qt, et, f64(x).T, fmt, block_rows, "qt")
+    for one in ("q", "qt"):  # each by itself gives the same
+        q2, e2 = (room8(rows, cols, fmt), scale_room(-(-rows // block_rows), cols)) if one == "q" else \
+            (room8(cols, rows, fmt), scale_room(-(-cols // block_rows), rows))
+        LU.layup_quant_fp8(LU.quant_desc(x, block_rows, **({"q": q2, "scale": e2} if one == "q" else {"qt": q2, "scale_t": e2})), s)
+        torch.cuda.synchronize()
+        a, b = (q, e) if one == "q" else (qt, et)
+        assert torch.equal(whole(q2).view(torch.uint8), whole(a).view(torch.uint8)) and torch.equal(whole(e2), whole(e if one == "q" else et))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("d", [1, 100, 128, 768, 1000, 1024, 1500, 4000, 8192, 16384])
+def test_norm_in_8_bits(fmt, d):
+    """The 8-bit y is the quantisation of the float32 y that the same call gives, byte for byte."""
+    rng = np.random.default_rng(d)
+    rows = 7
+    x, r = matrix(rng, rows, d, BF16), matrix(rng, rows, d, F32)
+    g, b = (torch.from_numpy(rng.normal(size=d)).float().to(DEV) for _ in range(2))
+    y, q, e = torch.empty(rows, d, device=DEV), room8(rows, d, fmt), scale_room(rows, d)
+    kw = dict(residual=r, p=0.1, seed=3)
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, y, g, b, **kw))
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, q, g, b, y_scale=e, **kw))
+    torch.cuda.synchronize()
+    check_quant(q, e, f64(y), fmt, 1, "y")
+
+
+def quantised(x, block_rows, fmt):
+    rows, k = x.shape
+    q, e = room8(rows, k, fmt), scale_room(-(-rows // block_rows), k)
+    LU.layup_quant_fp8(LU.quant_desc(x, block_rows, q=q, scale=e), torch.cuda.current_stream())
+    return q, e
+
+
+def values(q, e, k, block_rows):
+    nb = -(-k // 128)
+    v = q.view(torch.uint8)[:, :k].contiguous().view(q.dtype).double().cpu().numpy()
+    return R.value(v, e[:, :nb].cpu().numpy(), block_rows)
+
+
+def product_bound(va, vb, out):
+    """Products are exact.  A float32 sum of K of them is off by at most K u of the sum of absolute values, twice that
+    where the matrix unit truncates.  For a bfloat16 result the 8-bit unit also truncates each product to a multiple of
+    2^-13 of the power of two under the largest of its group of eight: seven errors below 2^-13 of that largest one,
+    bounded from above by the product of the largest factors."""
+    K = va.shape[1]
+    tol = 2 * (K + 8) * U * (np.abs(va) @ np.abs(vb).T)
+    if out == BF16:
+        pad = -K % 8
+        a, b = (torch.from_numpy(np.pad(np.abs(v), ((0, 0), (0, pad)))).to(DEV) for v in (va, vb))
+        # max over a group of a_k b_k <= max a_k max b_k
+        ga, gb = (v.reshape(v.shape[0], -1, 8).amax(2) for v in (a, b))
+        tol = tol + 7 * 2.0 ** -13 * (ga @ gb.t()).cpu().numpy()
+    return tol
+
+
+def product(M, N, K, fa="e4m3", fb="e4m3", ba=1, bb=128, out=BF16, bias=True, pad=0, ws=0, spread=1.0, seed=0):
+    rng = np.random.default_rng(seed + M + 3 * N + 7 * K)
+    a = (torch.from_numpy(rng.normal(size=(M, K))) * torch.exp(spread * torch.from_numpy(rng.normal(size=(M, 1))))).float().to(DEV)
+    b = torch.from_numpy(rng.normal(size=(N, K)) * 0.05).float().to(DEV)
+    (qa, ea), (qb, eb) = quantised(a, ba, fa), quantised(b, bb, fb)
+    c = matrix(rng, M, N, out, pad)
+    bvec = torch.from_numpy(rng.normal(size=N)).float().to(DEV) if bias else None
+    room = torch.full((ws,), 0x7f, dtype=torch.uint8, device=DEV) if ws else None
+    desc = LU.gemm_fp8_desc(qa, ea, ba, qb, eb, bb, c, K, bias=bvec, workspace=room)
+    LU.layup_gemm_fp8(desc, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    va, vb = values(qa, ea, K, ba), values(qb, eb, K, bb)
+    ref = va @ vb.T + (f64(bvec) if bias else 0.0)
+    tol = product_bound(va, vb, out) + U * (np.abs(ref) + (np.abs(f64(bvec)) if bias else 0.0))
+    near(f64(c), ref, tol + EPS[out] * (np.abs(ref) + tol), "product")
+    untouched(c)
+    return c, desc
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 128), (3, 5, 100), (16, 48, 256), (17, 33, 129), (32, 257, 512), (33, 64, 64),
+                                   (64, 512, 1000), (65, 100, 2048), (128, 128, 128), (200, 136, 640), (257, 300, 384),
+                                   (1101, 523, 1000), (520, 1000, 1101)])
+@pytest.mark.parametrize("out,bias", [(BF16, True), (F32, False)])
+def test_product_shapes(M, N, K, out, bias):
+    product(M, N, K, out=out, bias=bias, pad=(M + N) % 3)
+
+
+@pytest.mark.parametrize("fa", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("fb", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("ba,bb", [(1, 1), (1, 128), (128, 1), (128, 128)])
+@pytest.mark.parametrize("M,N,K", [(5, 200, 384), (300, 260, 700)])
+def test_product_formats_and_blocks(fa, fb, ba, bb, M, N, K):
+    product(M, N, K, fa, fb, ba, bb, out=F32, spread=3.0)
+
+
+@pytest.mark.parametrize("M,N,K", [(768, 256, 8192), (96, 130, 5000), (4, 256, 8192), (1, 2048, 4096)])
+def test_product_long_k_with_workspace(M, N, K):
+    """With a workspace K may be split: within the same bound, and the same bits every time."""
+    a, desc = product(M, N, K, out=F32, ws=64 << 20)
+    first = a.clone()
+    for _ in range(3):
+        a.zero_()
+        LU.layup_gemm_fp8(desc, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(a, first)
+    product(M, N, K, out=BF16, ws=64 << 20)
+
+
+def test_product_large():
+    """2048 x 2304 x 768 and a wide one, on sampled rows and columns of the float64 product."""
+    for M, N, K in ((2048, 2304, 768), (1024, 8192, 2048)):
+        product(M, N, K, out=BF16)
+
+
+def test_product_of_no_k_is_the_bias():
+    c = torch.full((5, 9), 7.0, device=DEV)
+    b = torch.arange(9, dtype=F32, device=DEV)
+    d = LU.layup_gemm_fp8_desc(M=5, N=9, K=0, C=c.data_ptr(), ldc=9, bias=b.data_ptr(), a_dtype=2, b_dtype=2, a_block=1, b_block=1, c_f32=1)
+    LU.layup_gemm_fp8(d)
+    torch.cuda.synchronize()
+    assert torch.equal(c, b.expand(5, 9))
+
+
+@pytest.mark.parametrize("M", [3, 70])
+def test_product_keeps_nan_in_its_row(M):
+    x = torch.randn(M, 300, device=DEV)
+    x[1, 200] = float("inf")
+    w = torch.randn(40, 300, device=DEV)
+    (qa, ea), (qb, eb) = quantised(x, 1, "e4m3"), quantised(w, 128, "e4m3")
+    c = torch.empty(M, 40, device=DEV)
+    LU.layup_gemm_fp8(LU.gemm_fp8_desc(qa, ea, 1, qb, eb, 128, c, 300))
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(c[1]).all()) and bool(torch.isfinite(c[0]).all()) and bool(torch.isfinite(c[2:]).all())
+
+
+# ----------------------------------------------------- a run of them together
+
+
+def test_a_layer_forward_and_backward_in_a_graph():
+    """s = residual + dropout(x); y = LN(s) in 8 bits; o = y W^T + b; and back: dW, dy, ds, dx, dgamma, dbeta.  On a
+    stream of its own, captured and replayed with new inputs; each stage against the reference from the values that the
+    stage before stored."""
+    rng = np.random.default_rng(12)
+    rows, d, n, p, seed = 200, 392, 264, 0.2, 77
+    x, r, do = matrix(rng, rows, d, BF16), matrix(rng, rows, d, F32), matrix(rng, rows, n, BF16, 0, 0.01)
+    w = matrix(rng, n, d, BF16, 0, 0.05)
+    g, b = (torch.from_numpy(1 + 0.1 * rng.normal(size=d)).float().to(DEV) for _ in range(2))
+    bias = torch.from_numpy(rng.normal(size=n)).float().to(DEV)
+    s, y, mean, rstd = (torch.empty(rows, d, device=DEV), torch.empty(rows, d, device=DEV, dtype=BF16), torch.empty(rows, device=DEV),
+                        torch.empty(rows, device=DEV))
+    o, dy, dres, dx = (torch.empty(rows, k, device=DEV, dtype=t) for k, t in ((n, BF16), (d, F32), (d, F32), (d, BF16)))
+    dw, dg, db = torch.empty(n, d, device=DEV), torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+    y8, ye = room8(rows, d, "e4m3"), scale_room(rows, d)
+    yt, yte = room8(d, rows, "e4m3"), scale_room(d, rows)
+    w8, we, wt, wte = room8(n, d, "e4m3"), scale_room(-(-n // 128), d), room8(d, n, "e4m3"), scale_room(-(-d // 128), n)
+    g8, ge, gt, gte = room8(rows, n, "e5m2"), scale_room(rows, n), room8(n, rows, "e5m2"), scale_room(n, rows)
+    counter = torch.zeros(1, dtype=torch.int64, device=DEV)
+    drop = dict(p=p, seed=seed, offset_dev=counter)
+    ws = torch.empty(max(16, LU.layup_layernorm_workspace_size(rows, d)), dtype=torch.uint8, device=DEV)
+    room = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    calls = [
+        (LU.layup_layernorm_forward, LU.layernorm_desc(x, y8, g, b, residual=r, sum_out=s, mean=mean, rstd=rstd, y_scale=ye, **drop)),
+        (LU.layup_layernorm_forward, LU.layernorm_desc(x, y, g, b, residual=r, **drop)),
+        (LU.layup_quant_fp8, LU.quant_desc(y, 1, qt=yt, scale_t=yte)),
+        (LU.layup_quant_fp8, LU.quant_desc(w, 128, q=w8, scale=we, qt=wt, scale_t=wte)),
+        (LU.layup_gemm_fp8, LU.gemm_fp8_desc(y8, ye, 1, w8, we, 128, o, d, bias=bias, workspace=room)),
+        (LU.layup_quant_fp8, LU.quant_desc(do, 1, q=g8, scale=ge, qt=gt, scale_t=gte)),
+        (LU.layup_gemm_fp8, LU.gemm_fp8_desc(g8, ge, 1, wt, wte, 128, dy, n, workspace=room)),
+        (LU.layup_gemm_fp8, LU.gemm_fp8_desc(gt, gte, 1, yt, yte, 1, dw, rows, workspace=room)),
+        (LU.layup_layernorm_backward, LU.layernorm_grad_desc(dy, s, mean, rstd, g, dres=dres, dx=dx, dgamma=dg, dbeta=db, workspace=ws, **drop)),
+    ]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    outs = dict(s=s, o=o, dy=dy, dw=dw, dres=dres, dx=dx, dg=dg, db=db)
+
+    def eager():
+        for call, desc in calls:
+            call(desc, stream)
+        stream.synchronize()
+        return {k: v.clone() for k, v in outs.items()}
+
+    with torch.cuda.stream(stream):
+        eager()
+        with torch.cuda.graph(graph, stream=stream):
+            cap = torch.cuda.current_stream()
+            for call, desc in calls:
+                call(desc, cap)
+    torch.cuda.synchronize()
+    for k in range(3):
+        x.copy_(torch.from_numpy(rng.normal(size=(rows, d))))
+        counter.fill_(k)
+        torch.cuda.synchronize()
+        want = eager()
+        for v in outs.values():
+            v.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, v in outs.items():
+            assert torch.equal(v, want[name]), (k, name)
+        # stage by stage
+        es = R.dropout(f64(x), p, seed, k) + f64(r)
+        near(f64(s), es, 4 * U * (np.abs(es) + 2 * np.abs(f64(x))), "s")
+        va, vw = values(y8, ye, d, 1), values(w8, we, d, 128)
+        yref, _, _ = R.norm_fwd(f64(s), f64(g), f64(b), 1e-5)
+        near(va, yref, 2.0 ** -4 * np.abs(yref) + 2.0 ** -14 * np.abs(yref).max() + 1e-5, "y in 8 bits")
+        tol = lambda a, b, c, t: product_bound(a, b, t) + 2 * U * (np.abs(c) + 4)  # noqa: E731
+        ref = va @ vw.T + f64(bias)
+        near(f64(o), ref, tol(va, vw, ref, BF16) * 1.01 + 2.0 ** -8 * np.abs(ref), "o")
+        vg, vt = values(g8, ge, n, 1), values(wt, wte, n, 128)
+        ref = vg @ vt.T
+        near(f64(dy), ref, tol(vg, vt, ref, F32), "dy")
+        vgt, vyt = values(gt, gte, rows, 1), values(yt, yte, rows, 1)
+        ref = vgt @ vyt.T
+        near(f64(dw), ref, tol(vgt, vyt, ref, F32), "dW")
+        refs = backward_ref(f64(dy), f64(s), f64(mean), f64(rstd), f64(g), 0.0 * f64(s), p, seed, k)
+        for name, (ref, t) in zip(("dres", "dx", "dg", "db"), refs):
+            near(f64(outs[name]), ref, t + EPS[outs[name].dtype] * (np.abs(ref) + t), name)
+
+
+def test_calls_on_two_streams_do_not_meet():
+    """The same calls on two streams at once, each with buffers of its own, give what one alone gives."""
+    rows, d, n = 512, 1024, 512
+    x = torch.randn(rows, d, device=DEV)
+    w = torch.randn(n, d, device=DEV)
+    sets = []
+    for _ in range(2):
+        q, e = room8(rows, d, "e4m3"), scale_room(rows, d)
+        w8, we = room8(n, d, "e4m3"), scale_room(n // 128, d)
+        c, y = torch.empty(rows, n, device=DEV), torch.empty(rows, d, device=DEV)
+        mean, rstd, dx, dg = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, d, device=DEV), torch.empty(d, device=DEV)
+        ws = torch.empty(LU.layup_layernorm_workspace_size(rows, d), dtype=torch.uint8, device=DEV)
+        room = torch.empty(8 << 20, dtype=torch.uint8, device=DEV)
+        calls = [(LU.layup_quant_fp8, LU.quant_desc(x, 1, q=q, scale=e)), (LU.layup_quant_fp8, LU.quant_desc(w, 128, q=w8, scale=we)),
+                 (LU.layup_gemm_fp8, LU.gemm_fp8_desc(q, e, 1, w8, we, 128, c, d, workspace=room)),
+                 (LU.layup_layernorm_forward, LU.layernorm_desc(x, y, mean=mean, rstd=rstd)),
+                 (LU.layup_layernorm_backward, LU.layernorm_grad_desc(y, x, mean, rstd, dx=dx, dgamma=dg, workspace=ws))]
+        sets.append((torch.cuda.Stream(), calls, (c, y, dx, dg)))
+    torch.cuda.synchronize()
+    for call, desc in sets[0][1]:
+        call(desc, sets[0][0])
+    torch.cuda.synchronize()
+    want = [t.clone() for t in sets[0][2]]
+    for _ in range(10):
+        for k in range(len(sets[0][1])):
+            for stream, calls, _ in sets:
+                calls[k][0](calls[k][1], stream)
+    torch.cuda.synchronize()
+    for _, _, outs in sets:
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
