@@ -627,7 +627,7 @@ layup_status layup_quant_fp8(const layup_quant_desc* d, void* stream);
  * W [out, in]: the forward is A = x, B = W; dX is A = dY, B = W^T (quantised
  * over out); dW is A = dY^T, B = x^T (both quantised over the tokens).  Each
  * operand is E4M3 or E5M2.  lda, ldb: at least K rounded up to 128, multiples
- * of 16; A and B 16-byte aligned; scales as layup_quant_fp8 states (bytes 1 to
+ * of 16, at most 2^24 (as the scales' rows); A and B 16-byte aligned; scales as layup_quant_fp8 states (bytes 1 to
  * 254).
  * workspace (device, optional, 16-byte aligned): float32 split-K partials; K is
  * split only when they fit, and the summation order, and so the rounding, then

@@ -23,7 +23,7 @@
 // too few tiles.  Causal attention products skip the tiles and K ranges that
 // the mask makes zero.  Epilogues fuse bias, residual add, GELU (storing the
 // pre-activation and the activation) and the GELU backward.
-#include "layup_internal.h"
+#include "lds_pipe.h"
 
 namespace layup {
 
@@ -240,7 +240,6 @@ __device__ __forceinline__ int mm_off(int kk, int c) { return kk * 2 * ROWS + 16
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef short v8i16 __attribute__((ext_vector_type(8)));
-#define LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
 
 // Issue copy i (of BLOCKS / NWAVES) of this wave's share of the
 // direct-to-LDS copies of one ROWS x BKV tile: one 1 KB block.
@@ -294,13 +293,6 @@ __device__ __forceinline__ const char* block_src(const bf16_t* base, int64_t ld,
   }
 }
 
-// One 1 KB block, 16 bytes per lane.  (A function template: the builtin's
-// width is checked against the target, and the host pass has none.)
-template <int>
-__device__ __forceinline__ void copy_block(const char* src, char* lds) {
-  __builtin_amdgcn_global_load_lds(src, LDS_PTR(lds), 16, 0, 0);
-}
-
 // Zero the k >= krem part of a tile (last, partial K step).
 template <int ROWS, bool KMAJOR, int BKV>
 __device__ __forceinline__ void zero_tail(char* lds, int krem) {
@@ -325,28 +317,6 @@ __device__ __forceinline__ void zero_tail(char* lds, int krem) {
 // flight into other stages, and before a transposing read it would wait for
 // every outstanding copy (vmcnt(0)), which serializes the copy pipeline.
 // Offsets are compile-time immediates where they are lane-independent.
-template <int N>
-struct IntC { static constexpr int value = N; };
-template <int I, int N, typename F>
-__device__ __forceinline__ void static_for(F&& f) {
-  if constexpr (I < N) {
-    f(IntC<I>{});
-    static_for<I + 1, N>(f);
-  }
-}
-
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-
-template <int OFF>
-__device__ __forceinline__ u32x4 lds_read_b128(uint32_t a) {
-  static_assert(OFF >= 0 && OFF < 65536, "LDS immediate offset");
-  u32x4 v;
-  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
-  return v;
-}
-
 template <int OFF>
 __device__ __forceinline__ u32x2 lds_read_tr(uint32_t a) {
   static_assert(OFF >= 0 && OFF < 65536, "LDS immediate offset");
@@ -354,15 +324,6 @@ __device__ __forceinline__ u32x2 lds_read_tr(uint32_t a) {
   asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
   return v;
 }
-
-// Wait until at most N LDS reads are outstanding (LDS reads return in order).
-template <int N>
-__device__ __forceinline__ void lgkm_wait() {
-  asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N < 15 ? N : 15));
-}
-
-// Make the MFMA that consumes v depend on the preceding wait.
-__device__ __forceinline__ void after_wait(u32x4& v) { asm volatile("" : "+v"(v)); }
 
 // Per-lane part of the LDS offset of a fragment.  k-major: one value per
 // K sub-step (the 32-row blocks are whole-row multiples apart, which the
@@ -394,18 +355,6 @@ __device__ __forceinline__ void read_frags(uint32_t sb, const uint32_t* off, u32
       f[i] = u32x4{lo.x, lo.y, hi.x, hi.y};
     }
   });
-}
-
-// s_waitcnt vmcnt(n), expcnt and lgkmcnt left alone (gfx9 encoding).
-#define WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4) | (15 << 8))
-
-// Workgroup barrier without the release fence of __syncthreads(): the fence
-// would make the compiler drain every outstanding direct-to-LDS load
-// (vmcnt(0)) at each K step; the exact wait is issued by hand before it.
-__device__ __forceinline__ void barrier_only() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 // WGM x WGN waves per workgroup; each wave owns a (BM/WGM) x (BN/WGN) block of
@@ -753,15 +702,6 @@ __device__ __forceinline__ void gemm_item(const KArgs& P, int lid) {
       __builtin_amdgcn_wave_barrier();
     }
   }
-}
-
-// The logical work item of a hardware workgroup.  The grid is one dimension
-// of n work items, padded to a multiple of 8.  Workgroups are dealt round-robin
-// over the 8 XCDs (each with its own L2), so hardware id h runs on XCD h % 8:
-// the remap gives every XCD a contiguous range of logical ids, i.e. whole
-// bands of tiles of one batch/split that share operand rows.
-__device__ __forceinline__ int work_item(int n, int h) {
-  return (h & 7) * ((n + 7) >> 3) + (h >> 3);
 }
 
 // OCC: workgroups per CU.

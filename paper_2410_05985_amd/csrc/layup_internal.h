@@ -284,6 +284,7 @@ hipError_t launch_norm_bwd(const layup_layernorm_grad_desc& d, const Mask& k, hi
 int64_t norm_partial_floats(int64_t rows, int d);
 hipError_t launch_quant_fp8(const layup_quant_desc& d, hipStream_t s);
 hipError_t launch_gemm_fp8(const layup_gemm_fp8_desc& d, hipStream_t s);
+hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits, hipStream_t s);
 
 // Records the text of a context-free call's error; returns st.  (model.hip)
 layup_status global_fail(layup_status st, const std::string& msg);
@@ -303,4 +304,6 @@ int layup_test_gelu(const float* x, float* y, float* dy, int64_t n, void* stream
 // given, holds the tensors of the update epilogue, one per product.
 int layup_test_gemm_tile(const layup_gemm_desc* d, int32_t n, int32_t group, int32_t cfg, int32_t splits,
                          int64_t run, const layup_tensor* upd, const layup_hparams* hp, float alpha, void* stream);
+// An 8-bit product with the tile configuration and split of K given; cfg < 0: the plan the library chooses.
+int layup_test_gemm_fp8_tile(const layup_gemm_fp8_desc* d, int32_t cfg, int32_t splits, void* stream);
 }

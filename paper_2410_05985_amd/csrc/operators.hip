@@ -187,7 +187,7 @@ layup_status layup_quant_fp8(const layup_quant_desc* d, void* stream) {
   });
 }
 
-layup_status layup_gemm_fp8(const layup_gemm_fp8_desc* d, void* stream) {
+static layup_status gemm_fp8(const layup_gemm_fp8_desc* d, int cfg, int splits, void* stream) {
   return call(d, stream, "8-bit product", [&](hipStream_t s) {
     const int64_t top = 1ll << 31;
     need(d->M >= 0 && d->N >= 0 && d->K >= 0 && d->M < top && d->N < top && d->K < top, LAYUP_ERR_SHAPE,
@@ -203,10 +203,19 @@ layup_status layup_gemm_fp8(const layup_gemm_fp8_desc* d, void* stream) {
       matrix8(d->B, d->ldb, d->K);
       scales(d->a_scale, d->ld_a_scale, d->K);
       scales(d->b_scale, d->ld_b_scale, d->K);
+      const int64_t most = 1ll << 24;  // 32-bit offsets inside a tile
+      need(d->lda <= most && d->ldb <= most && d->ld_a_scale <= most && d->ld_b_scale <= most, LAYUP_ERR_SHAPE,
+           "leading dimensions above 2^24 are not supported");
     }
     need(aligned(d->workspace, 16), LAYUP_ERR_ALIGN, "workspace must be 16-byte aligned");
-    return launch_gemm_fp8(*d, s);
+    return cfg < 0 ? launch_gemm_fp8(*d, s) : launch_gemm_fp8_cfg(*d, cfg, splits, s);
   });
+}
+
+layup_status layup_gemm_fp8(const layup_gemm_fp8_desc* d, void* stream) { return gemm_fp8(d, -1, 1, stream); }
+
+int layup_test_gemm_fp8_tile(const layup_gemm_fp8_desc* d, int32_t cfg, int32_t splits, void* stream) {
+  return gemm_fp8(d, cfg, splits, stream);
 }
 
 }  // extern "C"

@@ -402,7 +402,14 @@ def product_bound(va, vb, out):
     return tol
 
 
-def product(M, N, K, fa="e4m3", fb="e4m3", ba=1, bb=128, out=BF16, bias=True, pad=0, ws=0, spread=1.0, seed=0):
+def tile_call(desc, cfg, splits):
+    import ctypes
+    f = LU.lib().layup_test_gemm_fp8_tile
+    f.argtypes, f.restype = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p], ctypes.c_int
+    LU._check(f(ctypes.byref(desc), cfg, splits, LU._stream(torch.cuda.current_stream())))
+
+
+def product(M, N, K, fa="e4m3", fb="e4m3", ba=1, bb=128, out=BF16, bias=True, pad=0, ws=0, spread=1.0, seed=0, cfg=-1, splits=1):
     rng = np.random.default_rng(seed + M + 3 * N + 7 * K)
     a = (torch.from_numpy(rng.normal(size=(M, K))) * torch.exp(spread * torch.from_numpy(rng.normal(size=(M, 1))))).float().to(DEV)
     b = torch.from_numpy(rng.normal(size=(N, K)) * 0.05).float().to(DEV)
@@ -411,7 +418,10 @@ def product(M, N, K, fa="e4m3", fb="e4m3", ba=1, bb=128, out=BF16, bias=True, pa
     bvec = torch.from_numpy(rng.normal(size=N)).float().to(DEV) if bias else None
     room = torch.full((ws,), 0x7f, dtype=torch.uint8, device=DEV) if ws else None
     desc = LU.gemm_fp8_desc(qa, ea, ba, qb, eb, bb, c, K, bias=bvec, workspace=room)
-    LU.layup_gemm_fp8(desc, torch.cuda.current_stream())
+    if cfg < 0:
+        LU.layup_gemm_fp8(desc, torch.cuda.current_stream())
+    else:
+        tile_call(desc, cfg, splits)
     torch.cuda.synchronize()
     va, vb = values(qa, ea, K, ba), values(qb, eb, K, bb)
     ref = va @ vb.T + (f64(bvec) if bias else 0.0)
@@ -448,6 +458,24 @@ def test_product_long_k_with_workspace(M, N, K):
         torch.cuda.synchronize()
         assert torch.equal(a, first)
     product(M, N, K, out=BF16, ws=64 << 20)
+
+
+TILES = {"256x256": 0, "256x128": 1, "128x128": 2, "64x64": 3}
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("M,N,K,splits", [(1, 1, 1, 1), (300, 260, 128, 1), (300, 260, 256, 1), (270, 530, 384, 1),
+                                          (130, 72, 512, 1), (257, 300, 640, 2), (520, 516, 1408, 3), (100, 100, 8192, 16)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_product_tiles(tile, M, N, K, splits, out):
+    """Every tile by name: one step to many, edges, splits of K down to one block of 512."""
+    product(M, N, K, "e4m3", "e5m2", 1, 128 if out == BF16 else 1, out=out, pad=M % 3, ws=splits * M * N * 4 if splits > 1 else 0,
+            cfg=TILES[tile], splits=splits)
+
+
+def test_product_tile_refuses_too_small_a_workspace():
+    with pytest.raises(LU.LayupError):
+        product(64, 64, 1024, ws=64 * 64 * 4, cfg=3, splits=2)
 
 
 def test_product_large():

@@ -86,7 +86,8 @@ CASES = [
     (gemm, dict(ldc=7), SHAPE), (gemm, dict(C=0x5001), ALIGN), (gemm, dict(c_f32=1, C=0x5002), ALIGN), (gemm, dict(bias=0x6002), ALIGN),
     (gemm, dict(A=None), INVALID), (gemm, dict(B=None), INVALID), (gemm, dict(lda=16), SHAPE), (gemm, dict(ldb=130), ALIGN),
     (gemm, dict(A=0x1008), ALIGN), (gemm, dict(a_scale=None), INVALID), (gemm, dict(b_scale=0x4001), ALIGN),
-    (gemm, dict(ld_a_scale=6), ALIGN), (gemm, dict(K=513, lda=640, ldb=640), SHAPE), (gemm, dict(workspace=0x6004), ALIGN),
+    (gemm, dict(ld_a_scale=6), ALIGN), (gemm, dict(K=513, lda=640, ldb=640), SHAPE), (gemm, dict(lda=(1 << 24) + 16), SHAPE),
+    (gemm, dict(ld_b_scale=(1 << 24) + 4), SHAPE), (gemm, dict(workspace=0x6004), ALIGN),
 ]
 
 
