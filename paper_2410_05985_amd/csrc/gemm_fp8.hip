@@ -59,12 +59,29 @@ struct Frag {
   u32x4 lo, hi;
 };
 
-// acc += A B^T over the 64 k of two fragments; the scales are the low bytes.
-template <int FA, int FB, bool EXACT>
+__device__ __forceinline__ i32x8 words(const Frag& f) {
+  return i32x8{(int)f.lo[0], (int)f.lo[1], (int)f.lo[2], (int)f.lo[3], (int)f.hi[0], (int)f.hi[1], (int)f.hi[2], (int)f.hi[3]};
+}
+
+// acc += (A B^T)^T over the 64 k of two fragments; the scales are the low
+// bytes.  The accumulator holds the transposed block: lane l, register r is
+// column (r/4)*8 + (l/32)*4 + r%4 of row l%32 of C, so a lane has four
+// neighbouring columns in a row.
+template <int FA, int FB>
 __device__ __forceinline__ void product64(const Frag& a, const Frag& b, uint32_t sa, uint32_t sb, f32x16& acc) {
-  const i32x8 x{(int)a.lo[0], (int)a.lo[1], (int)a.lo[2], (int)a.lo[3], (int)a.hi[0], (int)a.hi[1], (int)a.hi[2], (int)a.hi[3]};
-  const i32x8 y{(int)b.lo[0], (int)b.lo[1], (int)b.lo[2], (int)b.lo[3], (int)b.hi[0], (int)b.hi[1], (int)b.hi[2], (int)b.hi[3]};
-  acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, FA, FB, 0, (int)sa, 0, (int)sb);
+  acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(words(b), words(a), acc, FB, FA, 0, (int)sb, 0, (int)sa);
+}
+
+// Moves the odd 16-lane (32-lane) groups of a with the even ones of b.
+__device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+__device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
 }
 
 // ------------------------------------------------------------------ tiles
@@ -77,6 +94,17 @@ __device__ __forceinline__ void product64(const Frag& a, const Frag& b, uint32_t
 // r*128 + 16*(c ^ ((r >> 1) & 7)): sixteen lanes reading one chunk of sixteen
 // consecutive rows cover all banks.
 //
+// Scale bytes: those of the tile's rows for SCN steps are copied to LDS before
+// the first one, as words of four steps; every step reads its words.  Row r has
+// SCN / 4 words, word w at place w ^ sc_swz(r), so that 32 consecutive rows'
+// words of a step lie in different banks.  (Fetched by the step, a word for
+// each row is a cache line for each row, as many requests as the operands
+// themselves: the copies alone took 446 us of 8192 x 8192 x 8192, now 399.
+// Kept in registers and loaded every fourth step, they brought a branch into
+// the step, over which the compiler moved the products it was to overlap, and
+// a wait for every copy in flight.)  A longer K drains the pipeline every SCN
+// steps.
+//
 // A step's products go in clusters of CA blocks of rows by all TN of columns
 // and 64 k, whose fragments are read while the cluster before is multiplied.
 // A step starts with the last cluster of the step before, already in
@@ -84,15 +112,21 @@ __device__ __forceinline__ void product64(const Frag& a, const Frag& b, uint32_t
 // fragment reads' latency and carry the copies of a later step.
 __device__ __forceinline__ int chunk_off(int r, int c) { return r * 128 + 16 * (c ^ ((r >> 1) & 7)); }
 
+// W words a row: 64 / W rows fill the banks once
+template <int W>
+__device__ __forceinline__ int sc_swz(int r) { return (r & 31) / (64 / W); }
+
 template <int BM, int BN, int WGM, int WGN, int S, int FA, int FB, bool EXACT>
 __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
   constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
   constexpr int LOADS_A = BM / 8 / NW, LOADS_B = BN / 8 / NW, NPIECE = LOADS_A + LOADS_B;
+  constexpr int SCN = 32, W = SCN / 4, ROWS = BM + BN, LOADS_S = ROWS * W / 64 / NW;  // scale words a row, copies a wave
+  static_assert(ROWS * W % (64 * NW) == 0, "copies of scales split evenly over the waves");
   static_assert(BM / 8 % NW == 0 && BN / 8 % NW == 0, "copies must split evenly over the waves");
   constexpr int CA = TM >= 2 ? 2 : 1, NC = TM / CA;  // clusters of 64 k
   static_assert(TM % CA == 0, "whole clusters");
-  __shared__ __attribute__((aligned(1024))) char smem[S * (A_BYTES + B_BYTES)];
+  __shared__ __attribute__((aligned(1024))) char smem[S * (A_BYTES + B_BYTES) + ROWS * SCN];
 
   // tiles go in groups of 8 tile-rows for L2 reuse of B
   const int n_tiles = P.tiles_m * P.tiles_n;
@@ -134,30 +168,31 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   auto issue = [&](int slot, int p) {  // copy p of the next step into a stage
     if (p < LOADS_A) copy_block<0>(base_a + off_a[p], smem + slot * A_BYTES + (wave * LOADS_A + p) * 1024);
     else copy_block<0>(base_b + off_b[p - LOADS_A], smem_b + slot * B_BYTES + (wave * LOADS_B + p - LOADS_A) * 1024);
-    if (p == LOADS_A - 1) base_a += 128;
-    if (p == NPIECE - 1) base_b += 128;
+    if (p == NPIECE - 1) {
+      base_a += 128;
+      base_b += 128;
+    }
   };
-
-  // scale bytes, four steps to a word: sa, sb the words in use (the low byte
-  // is the step's), na, nb the next ones
-  uint32_t sa[TM], sb[TN], na[TM], nb[TN], wa[TM], wb[TN];
-  const int64_t ma = m0 >> P.fa, mb = n0 >> P.fb;
-  const uint32_t* base_sa = reinterpret_cast<const uint32_t*>(P.sa + ma * P.ldsa + kb0);
-  const uint32_t* base_sb = reinterpret_cast<const uint32_t*>(P.sb + mb * P.ldsb + kb0);
+  // the scale words of steps k0 .. k0 + SCN - 1; past the last one, that again
+  char* const smem_s = smem + S * (A_BYTES + B_BYTES);
+  auto copy_scales = [&](int k0) {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // no addresses kept in registers for a next round
+    const int last = (min(nk - k0, SCN) - 1) >> 2;
+    const int in_a = (int)(m0 & ((1 << P.fa) - 1)), in_b = (int)(n0 & ((1 << P.fb) - 1));  // rows into the first block
+    const char* sa0 = (const char*)P.sa + (m0 >> P.fa) * P.ldsa + kb0 + k0;
+    const char* sb0 = (const char*)P.sb + (n0 >> P.fb) * P.ldsb + kb0 + k0;
+    const int max_a = (int)min(P.M - 1 - m0, (int64_t)BM), max_b = (int)min(P.N - 1 - n0, (int64_t)BN);
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t r = min(m0 + wm * WM + 32 * i + (lane & 31), P.M - 1);
-    wa[i] = (uint32_t)((r >> P.fa) - ma) * ((uint32_t)P.ldsa >> 2);
-    na[i] = base_sa[wa[i]];
-    sa[i] = 127;
-  }
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int64_t r = min(n0 + wn * WN + 32 * j + (lane & 31), P.N - 1);
-    wb[j] = (uint32_t)((r >> P.fb) - mb) * ((uint32_t)P.ldsb >> 2);
-    nb[j] = base_sb[wb[j]];
-    sb[j] = 127;
-  }
+    for (int i = 0; i < LOADS_S; ++i) {
+      const int t = (wave * LOADS_S + i) * 64, r0 = t / W, r = r0 + ln / W;
+      const int w = min((ln % W) ^ sc_swz<W>(r), last);
+      if (r0 < BM)  // uniform: a copy's rows are of one operand
+        copy_words<0>(sa0 + ((uint32_t)((min(r, max_a) + in_a) >> P.fa) * (uint32_t)P.ldsa + 4 * w), smem_s + t * 4);
+      else
+        copy_words<0>(sb0 + ((uint32_t)((min(r - BM, max_b) + in_b) >> P.fb) * (uint32_t)P.ldsb + 4 * w), smem_s + t * 4);
+    }
+  };
 
   // fragments: rows 32 i + lane % 32, chunks 2 ks + lane / 32; the swizzle
   // leaves whole blocks of 32 rows alone
@@ -168,6 +203,13 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     b_off[ks] = chunk_off(wn * WN + (lane & 31), 2 * ks + (lane >> 5));
   }
   const uint32_t lds0 = lds_addr(smem);
+  const uint32_t sa_off = lds0 + S * (A_BYTES + B_BYTES) + 4 * W * (wm * WM + (lane & 31));
+  const uint32_t sb_off = lds0 + S * (A_BYTES + B_BYTES) + 4 * W * (BM + wn * WN + (lane & 31));
+  uint32_t sa[TM], sb[TN], wa[TM], wb[TN];  // scales in use (the low byte counts); the words of the step that begins
+#pragma unroll
+  for (int i = 0; i < TM; ++i) sa[i] = 127;
+#pragma unroll
+  for (int j = 0; j < TN; ++j) sb[j] = 127;
   Frag af[2][CA], bf[2][TN];
 #pragma unroll
   for (int i = 0; i < CA; ++i) af[1][i].lo = af[1][i].hi = u32x4{0, 0, 0, 0};
@@ -175,9 +217,14 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   for (int j = 0; j < TN; ++j) bf[1][j].lo = bf[1][j].hi = u32x4{0, 0, 0, 0};
 
   // cluster q of a step: 64 k number q / NC, row blocks CA (q % NC) ..
-  auto read_cluster = [&](auto Q, int slot) {
+  auto read_cluster = [&](auto Q, int kt, int slot) {
     constexpr int q = decltype(Q)::value, h = q / NC, i0 = CA * (q % NC);
     const uint32_t ab = lds0 + (uint32_t)(slot * A_BYTES), bb = lds0 + (uint32_t)(S * A_BYTES + slot * B_BYTES);
+    if constexpr (q == 0) {
+      const uint32_t w = 4 * ((kt >> 2) ^ sc_swz<W>(lane));
+      static_for<0, TM>([&](auto I) { wa[decltype(I)::value] = lds_read_b32<decltype(I)::value * 128 * W>(sa_off + w); });
+      static_for<0, TN>([&](auto J) { wb[decltype(J)::value] = lds_read_b32<decltype(J)::value * 128 * W>(sb_off + w); });
+    }
     if constexpr (q % NC == 0)
       static_for<0, TN>([&](auto J) {
         constexpr int j = decltype(J)::value;
@@ -192,6 +239,12 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   };
   auto landed = [&](auto Q) {  // the cluster's reads have been waited for
     constexpr int q = decltype(Q)::value, h = q / NC;
+    if constexpr (q == 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) after_wait(wa[i]);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) after_wait(wb[j]);
+    }
     if constexpr (q % NC == 0)
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
@@ -225,7 +278,7 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
           const bf16x8 xa = widen<FA>(v[2 * (x & 1)], v[2 * (x & 1) + 1], scale_of(sa[i0 + i]));
 #pragma unroll
           for (int j = 0; j < TN; ++j)
-            acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa, xb[j], acc[i0 + i][j], 0, 0, 0);
+            acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j], xa, acc[i0 + i][j], 0, 0, 0);
         }
         if constexpr (copy) {
 #pragma unroll
@@ -238,7 +291,7 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
       for (int i = 0; i < CA; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-          product64<FA, FB, EXACT>(af[q & 1][i], bf[h & 1][j], sa[i0 + i], sb[j], acc[i0 + i][j]);
+          product64<FA, FB>(af[q & 1][i], bf[h & 1][j], sa[i0 + i], sb[j], acc[i0 + i][j]);
           if constexpr (copy) {
 #pragma unroll
             for (int p = (i * TN + j) * PER; p < (i * TN + j + 1) * PER; ++p)
@@ -250,121 +303,146 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     __builtin_amdgcn_sched_barrier(0);
   };
   auto advance = [&](int kt) {  // the scales of step kt
-    if ((kt & 3) == 0) {
-      const int g = min(kt + 4, (nk - 1) & ~3) >> 2;
+    const int sh = 8 * (kt & 3);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        sa[i] = na[i];
-        na[i] = base_sa[g + wa[i]];
-      }
+    for (int i = 0; i < TM; ++i) sa[i] = wa[i] >> sh;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        sb[j] = nb[j];
-        nb[j] = base_sb[g + wb[j]];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] >>= 8;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sb[j] >>= 8;
-    }
+    for (int j = 0; j < TN; ++j) sb[j] = wb[j] >> sh;
   };
   constexpr int LAST = 2 * NC - 1;
-  // reads outstanding that belong to the younger cluster
-  auto reads_of = [](int q) constexpr { return 2 * CA + (q % NC == 0 ? 2 * TN : 0); };
-  // MAIN: step kt + S - 1 exists.  No branch between LDS reads and their wait.
-  auto k_step = [&](auto MAIN, int kt, int slot) {
+  // MAIN: step kt + S - 1 of the ns exists.  No branch between LDS reads and
+  // their wait.
+  auto k_step = [&](auto MAIN, int kt, int ns, int slot) {
     constexpr bool main = decltype(MAIN)::value != 0;
     const int pslot = slot == 0 ? S - 1 : slot - 1;  // of steps kt - 1 and kt + S - 1
     if constexpr (main) {
       WAIT_VMCNT((S - 2) * NPIECE);  // loads complete in order: step kt has landed
     } else {
-      const int left = min(S - 2, nk - 1 - kt);  // younger steps still in flight
+      const int left = min(S - 2, ns - 1 - kt);  // younger steps still in flight
       static_for<0, S - 1>([&](auto D) {
         constexpr int d = decltype(D)::value;
         if (left == d) WAIT_VMCNT(d * NPIECE);
       });
     }
     barrier_only();
-    read_cluster(IntC<0>{}, slot);
+    read_cluster(IntC<0>{}, kt, slot);
     multiply(IntC<LAST>{}, IntC<main ? 1 : 0>{}, pslot);
     lgkm_wait<0>();
     landed(IntC<0>{});
     advance(kt);
     static_for<0, LAST>([&](auto Q) {
       constexpr int q = decltype(Q)::value;
-      read_cluster(IntC<q + 1>{}, slot);
+      read_cluster(IntC<q + 1>{}, kt, slot);
       multiply(Q, IntC<0>{}, 0);
       lgkm_wait<0>();
       landed(IntC<q + 1>{});
     });
   };
-  for (int t = 0; t < S - 1; ++t)
-    if (t < nk)
+  for (int k0 = 0; k0 < nk; k0 += SCN) {
+    const int ns = min(nk - k0, SCN);
+    if (k0 > 0) barrier_only();  // every wave has read the last stage
+    // the first stage before the scales, which the first step waits for too
 #pragma unroll
-      for (int p = 0; p < NPIECE; ++p) issue(t, p);
-  int kt = 0, slot = 0;
-  for (; kt + S - 1 < nk; ++kt) {
-    k_step(IntC<1>{}, kt, slot);
-    slot = slot + 1 == S ? 0 : slot + 1;
-  }
-  for (; kt < nk; ++kt) {
-    k_step(IntC<0>{}, kt, slot);
-    slot = slot + 1 == S ? 0 : slot + 1;
+    for (int t = 0; t < S - 1; ++t) {
+      if (t < ns)
+#pragma unroll
+        for (int p = 0; p < NPIECE; ++p) issue(t, p);
+      if (t == 0) copy_scales(k0);
+    }
+    int kt = 0, slot = 0;
+    for (; kt + S - 1 < ns; ++kt) {
+      k_step(IntC<1>{}, kt, ns, slot);
+      slot = slot + 1 == S ? 0 : slot + 1;
+    }
+    for (; kt < ns; ++kt) {
+      k_step(IntC<0>{}, kt, ns, slot);
+      slot = slot + 1 == S ? 0 : slot + 1;
+    }
   }
   multiply(IntC<LAST>{}, IntC<0>{}, 0);
 
-  // ---- epilogue.  32x32 accumulator layout: lane l, register r holds row
-  // (r/4)*8 + (l/32)*4 + r%4, column l%32.  Each block passes through a
-  // wave-private LDS buffer, after which a lane owns eight consecutive columns
-  // of one row (LDS requests of one wave are served in order).
-  constexpr int LDW = 40;  // floats per staged row: rows r and r + 4 sit 32 banks apart
-  static_assert(NW * 32 * LDW * 4 <= S * (A_BYTES + B_BYTES), "staging fits in the stages");
-  __syncthreads();  // every wave has finished reading the stages
-  float* const stg = reinterpret_cast<float*>(smem) + wave * 32 * LDW;
+  // ---- epilogue, from the registers.  A lane has columns 8 q + 4 (l/32) ..+3
+  // of row l%32 for q = 0..3; exchanges between lane groups gather 16 bytes of
+  // a row in a lane and 64 bytes of it in four lanes, so a store covers sixteen
+  // rows' 64-byte pieces.
   const bool part = P.splits > 1;
   const bool wide = part || EXACT;  // float32 stores
   float* const cf = part ? P.partial + (int64_t)split * P.M * P.N : (float*)P.C;
   const int64_t ldc = part ? P.N : P.ldc;
   const float* const bias = part ? nullptr : P.bias;
-  const bool vec = ((part ? (uintptr_t)P.partial : (uintptr_t)P.C) & 15) == 0 && (ldc & 7) == 0 && (P.N & 7) == 0 &&
-                   ((uintptr_t)bias & 15) == 0;
+  const bool vec = ((uintptr_t)(part ? (void*)P.partial : P.C) & 15) == 0 && (ldc & 7) == 0 && (P.N & 7) == 0;
+  const int hf = lane >> 5, l16 = (lane >> 4) & 1, l4 = lane & 15;
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int64_t nb = n0 + wn * WN + j * 32;
+    if (bias) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int64_t n = nb + 8 * q + 4 * hf + t;
+          const float x = n < P.N ? bias[n] : 0.f;
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][j][4 * q + t] += x;
+        }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
+    const int64_t mb = m0 + wm * WM + i * 32;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
+      const int64_t nb = n0 + wn * WN + j * 32;
+      if (!vec) {
+        const int64_t m = mb + (lane & 31);
+        if (m < P.M)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) stg[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * LDW + (lane & 31)] = acc[i][j][r];
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int it = 0; it < 2; ++it) {
-        const int rr = (lane + 64 * it) >> 2, cc = ((lane + 64 * it) & 3) * 8;
-        const int64_t m = m0 + wm * WM + i * 32 + rr, n = n0 + wn * WN + j * 32 + cc;
-        f32x4 v0 = *reinterpret_cast<const f32x4*>(stg + rr * LDW + cc), v1 = *reinterpret_cast<const f32x4*>(stg + rr * LDW + cc + 4);
-        if (m >= P.M || n >= P.N) continue;
-        if (vec) {
-          if (bias) {
-            v0 += *reinterpret_cast<const f32x4*>(bias + n);
-            v1 += *reinterpret_cast<const f32x4*>(bias + n + 4);
+          for (int r = 0; r < 16; ++r) {
+            const int64_t n = nb + 8 * (r >> 2) + 4 * hf + (r & 3);
+            if (n >= P.N) continue;
+            if (wide) cf[m * ldc + n] = acc[i][j][r];
+            else ((bf16_t*)P.C)[m * ldc + n] = f2bf(acc[i][j][r]);
           }
-          if (wide) {
-            *reinterpret_cast<f32x4*>(cf + m * ldc + n) = v0;
-            *reinterpret_cast<f32x4*>(cf + m * ldc + n + 4) = v1;
-          } else {
-            *reinterpret_cast<u32x4*>((bf16_t*)P.C + m * ldc + n) =
-                u32x4{pack_bf2(v0[0], v0[1]), pack_bf2(v0[2], v0[3]), pack_bf2(v1[0], v1[1]), pack_bf2(v1[2], v1[3])};
-          }
-        } else {
+      } else if (wide) {
+        // q pairs: columns 16 p .. + 15
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (n + e >= P.N) continue;
-            const float x = (e < 4 ? v0[e & 3] : v1[e & 3]) + (bias ? bias[n + e] : 0.f);
-            if (wide) cf[m * ldc + n + e] = x;
-            else ((bf16_t*)P.C)[m * ldc + n + e] = f2bf(x);
+        for (int p = 0; p < 2; ++p) {
+          uint32_t x[4], y[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const float u = acc[i][j][8 * p + t], v = acc[i][j][8 * p + 4 + t];
+            x[t] = __builtin_bit_cast(uint32_t, u);
+            y[t] = __builtin_bit_cast(uint32_t, v);
+            swap16(x[t], y[t]);  // x: rows 0..15, y: rows 16..31; odd lane groups: columns 8 ..
+          }
+          const int64_t n = nb + 16 * p + 8 * l16 + 4 * hf;
+          if (n < P.N) {
+            if (mb + l4 < P.M) *reinterpret_cast<u32x4*>(cf + (mb + l4) * ldc + n) = u32x4{x[0], x[1], x[2], x[3]};
+            if (mb + 16 + l4 < P.M) *reinterpret_cast<u32x4*>(cf + (mb + 16 + l4) * ldc + n) = u32x4{y[0], y[1], y[2], y[3]};
           }
         }
+      } else {
+        uint32_t w[2][4];  // columns 16 p + 8 (l/32) .. + 7 of row l%32
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const f32x16& v = acc[i][j];
+          w[p][0] = pack_bf2(v[8 * p], v[8 * p + 1]);
+          w[p][1] = pack_bf2(v[8 * p + 2], v[8 * p + 3]);
+          w[p][2] = pack_bf2(v[8 * p + 4], v[8 * p + 5]);
+          w[p][3] = pack_bf2(v[8 * p + 6], v[8 * p + 7]);
+          swap32(w[p][0], w[p][2]);
+          swap32(w[p][1], w[p][3]);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) swap16(w[0][t], w[1][t]);  // w[y]: row 16 y + l%16, columns 16 (l/16 odd) + 8 (l/32)
+        const int64_t n = nb + 16 * l16 + 8 * hf;
+        if (n < P.N)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int64_t m = mb + 16 * y + l4;
+            if (m < P.M) __builtin_nontemporal_store(u32x4{w[y][0], w[y][1], w[y][2], w[y][3]}, reinterpret_cast<u32x4*>((bf16_t*)P.C + m * ldc + n));
+          }
       }
-      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -376,6 +454,102 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC * WGM * WGN / 4) void gemm_fp8_
   const int lid = work_item(n, blockIdx.x);
   if (lid >= n) return;
   tile_item<BM, BN, WGM, WGN, S, FA, FB, EXACT>(P, lid);
+}
+
+// -------------------------------------------------------- few rows of A
+// M <= 32 (serving): bound by the stream of B, which goes from memory to the
+// matrix cores without LDS.  A workgroup takes 16 columns (16x16x128 products),
+// its waves share K in groups of four blocks (512 k, one word of scales a row),
+// a group's loads all in flight at once.  Of a block a lane takes the 16-byte
+// chunks l/16 and 4 + l/16 of row l%16, so a load covers 64 neighbouring bytes
+// of sixteen rows (with 32 columns and 32x32x64 products, 32 bytes of 32 rows:
+// 1 x 2048 x 8192 took 11.8 us).  The waves' sums meet in LDS and are added in
+// wave order.
+template <int TM, int FA, int FB, bool EXACT>
+__global__ __launch_bounds__(1024) void gemm_fp8_rows_kernel(const Fp8Args P) {
+  __shared__ float sums[16][TM * 4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t rb = min(n0 + (lane & 15), P.N - 1);
+  const uint8_t* b = P.B + rb * P.ldb + 16 * (lane >> 4);
+  const uint32_t* sb = reinterpret_cast<const uint32_t*>(P.sb + (rb >> P.fb) * P.ldsb);
+  const uint8_t* a[TM];
+  const uint32_t* sa[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t ra = min((int64_t)16 * i + (lane & 15), P.M - 1);
+    a[i] = P.A + ra * P.lda + 16 * (lane >> 4);
+    sa[i] = reinterpret_cast<const uint32_t*>(P.sa + (ra >> P.fa) * P.ldsa);
+  }
+  f32x4 acc[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto load = [](const uint8_t* p, int block) {
+    p += (int64_t)block * 128;
+    return Frag{*reinterpret_cast<const u32x4*>(p), *reinterpret_cast<const u32x4*>(p + 64)};
+  };
+  // a block's 128 k: lane l has column l%16 and rows 4 (l/16) .. + 3 of the sum
+  auto block = [&](const Frag& x, const Frag& y, uint32_t ea, uint32_t eb, f32x4& c) {
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const u32x4 &xv = h < 2 ? x.lo : x.hi, &yv = h < 2 ? y.lo : y.hi;
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FA>(xv[2 * (h & 1)], xv[2 * (h & 1) + 1], scale_of(ea)),
+                                                    widen<FB>(yv[2 * (h & 1)], yv[2 * (h & 1) + 1], scale_of(eb)), c, 0, 0, 0);
+      }
+    } else {
+      c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(words(x), words(y), c, FA, FB, 0, (int)ea, 0, (int)eb);
+    }
+  };
+  for (int g = wave; 4 * g < P.kb; g += nw) {
+    uint32_t wa[TM];
+    const uint32_t wb = sb[g];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) wa[i] = sa[i][g];
+    if (4 * g + 4 <= P.kb) {
+      Frag y[4], x[TM][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        y[k] = load(b, 4 * g + k);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) x[i][k] = load(a[i], 4 * g + k);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < TM; ++i) block(x[i][k], y[k], wa[i] >> (8 * k), wb >> (8 * k), acc[i]);
+    } else {
+      for (int k = 0; 4 * g + k < P.kb; ++k) {
+        const Frag y = load(b, 4 * g + k);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) block(load(a[i], 4 * g + k), y, wa[i] >> (8 * k), wb >> (8 * k), acc[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sums[wave][4 * i + r][lane] = acc[i][r];
+  __syncthreads();
+  for (int t = threadIdx.x; t < TM * 256; t += blockDim.x) {
+    const int i = t >> 8, r = (t >> 6) & 3, l = t & 63;
+    const int64_t m = 16 * i + 4 * (l >> 4) + r, n = n0 + (l & 15);
+    if (m >= P.M || n >= P.N) continue;
+    float v = 0.f;
+    for (int w = 0; w < nw; ++w) v += sums[w][4 * i + r][l];
+    if (P.bias) v += P.bias[n];
+    if (EXACT) ((float*)P.C)[m * P.ldc + n] = v;
+    else ((bf16_t*)P.C)[m * P.ldc + n] = f2bf(v);
+  }
+}
+
+template <int TM, int FA, int FB>
+hipError_t launch_rows(const Fp8Args& P, hipStream_t s) {
+  const int nw = (int)std::min<int64_t>(16, cdiv(P.kb, 4));
+  const unsigned grid = (unsigned)cdiv(P.N, 16);
+  if (P.c_f32) gemm_fp8_rows_kernel<TM, FA, FB, true><<<grid, 64 * nw, 0, s>>>(P);
+  else gemm_fp8_rows_kernel<TM, FA, FB, false><<<grid, 64 * nw, 0, s>>>(P);
+  return hipGetLastError();
 }
 
 // Sum of the split-K partials in split order, bias, rounding: four columns of
@@ -420,11 +594,44 @@ hipError_t launch_tiles(const Fp8Args& P, hipStream_t s) {
   return hipGetLastError();
 }
 
+enum TileId { T256x256 = 0, T256x128, T128x128, T64x64, T_ROWS, kNumCfg };
+// Estimate of a product's time.  occ workgroups share a CU; a step of 128 k
+// takes lo us alone on a CU and hi with the CU full (occ = 1: on an empty and
+// on a full chip), a tile fix us besides (first copies, stores), a byte of C
+// 1 / gbs ns.  Fitted to 1008 timings of 70 products of 65 to 8192 a side, with
+// operands and result in rotation: the choice takes 1.01 of the best tile and
+// split's time on average, 1.04 at the 90th percentile, 1.17 at most.  [0]:
+// bfloat16 results, [1]: float32.
 struct TileCfg {
-  int bm, bn;
+  int bm, bn, occ;
+  struct {
+    float lo, hi, fix, gbs;
+  } t[2];
 };
-enum TileId { T256x256 = 0, T256x128, T128x128, T64x64, kNumCfg };
-const TileCfg kCfgs[kNumCfg] = {{256, 256}, {256, 128}, {128, 128}, {64, 64}};
+const TileCfg kCfgs[kNumCfg] = {
+    {256, 256, 1, {{1.01f, 0.73f, 15.0f, 1300.f}, {2.27f, 2.02f, 15.4f, 1800.f}}},  // 2 x 4 waves, 2 stages
+    {256, 128, 1, {{0.59f, 0.44f, 7.5f, 1300.f}, {1.27f, 1.15f, 8.0f, 2000.f}}},    // 4 x 2 waves, 3 stages
+    {128, 128, 2, {{0.53f, 0.54f, 4.5f, 1220.f}, {0.76f, 1.21f, 5.2f, 1950.f}}},    // 2 x 2 waves, 2 stages
+    {64, 64, 4, {{0.37f, 0.55f, 1.6f, 1130.f}, {0.40f, 0.91f, 1.9f, 1970.f}}},      // 2 x 2 waves, 2 stages
+    {32, 16, 1, {}},
+};
+
+float estimate(int64_t M, int64_t N, int kb, bool f32, const TileCfg& c, int splits) {
+  const auto& t = c.t[f32];
+  int64_t steps = cdiv(kb, splits);
+  if (splits > 1) steps = cdiv(steps, 4) * 4;
+  splits = (int)cdiv(kb, steps);
+  const int64_t n = cdiv(M, c.bm) * cdiv(N, c.bn) * splits, q = cdiv(n, 256);  // tiles of the fullest CU
+  auto step = [&](int64_t k) {
+    const float x = c.occ > 1 ? (float)(k - 1) / (c.occ - 1) : std::min(1.f, n / 256.f);
+    return t.lo + (t.hi - t.lo) * x;
+  };
+  float us = (q / c.occ) * (steps * step(c.occ) + t.fix);
+  if (q % c.occ) us += steps * step(q % c.occ) + t.fix;
+  const float out = (float)M * N * (f32 ? 4.f : 2.f);
+  // the partial results are written and read at 4 TB/s, by one launch more
+  return splits > 1 ? us + 5.f + splits * (float)M * N * 8.f * 0.25e-6f : us + out * 1e-3f / t.gbs;
+}
 
 template <int FA, int FB>
 hipError_t launch_cfg(const Fp8Args& P, int cfg, hipStream_t s) {
@@ -432,7 +639,8 @@ hipError_t launch_cfg(const Fp8Args& P, int cfg, hipStream_t s) {
     case T256x256: return launch_tiles<256, 256, 2, 4, 2, 1, FA, FB>(P, s);
     case T256x128: return launch_tiles<256, 128, 4, 2, 3, 1, FA, FB>(P, s);
     case T128x128: return launch_tiles<128, 128, 2, 2, 2, 2, FA, FB>(P, s);
-    default: return launch_tiles<64, 64, 2, 2, 2, 4, FA, FB>(P, s);
+    case T64x64: return launch_tiles<64, 64, 2, 2, 2, 4, FA, FB>(P, s);
+    default: return P.M <= 16 ? launch_rows<1, FA, FB>(P, s) : launch_rows<2, FA, FB>(P, s);
   }
 }
 
@@ -473,7 +681,7 @@ hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits
     fp8_bias_kernel<<<(unsigned)cdiv(P.M * P.N, 256), 256, 0, s>>>(P);
     return hipGetLastError();
   }
-  if (cfg < 0 || cfg >= kNumCfg) return hipErrorInvalidValue;
+  if (cfg < 0 || cfg >= kNumCfg || (cfg == T_ROWS && (d.M > 32 || splits > 1))) return hipErrorInvalidValue;
   P.kb_split = (int32_t)(cdiv(cdiv(P.kb, std::max(1, splits)), 4) * 4);
   P.splits = (int32_t)cdiv(P.kb, P.kb_split);
   if (P.splits > 1 && (!d.workspace || d.workspace_bytes < (size_t)P.splits * P.M * P.N * 4)) return hipErrorInvalidValue;
@@ -485,9 +693,22 @@ hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits
 }
 
 hipError_t launch_gemm_fp8(const layup_gemm_fp8_desc& d, hipStream_t s) {
-  const int64_t t256 = cdiv(d.M, 256) * cdiv(d.N, 256), t128 = cdiv(d.M, 128) * cdiv(d.N, 128);
-  const int cfg = t256 >= 200 ? T256x256 : t128 >= 200 ? T128x128 : T64x64;
-  return launch_gemm_fp8_cfg(d, cfg, 1, s);
+  if (d.M <= 32) return launch_gemm_fp8_cfg(d, T_ROWS, 1, s);
+  const int kb = (int)cdiv(d.K, 128);
+  int cfg = T64x64, splits = 1;
+  float best = 1e30f;
+  for (int c = 0; c < T_ROWS; ++c)
+    for (int sp = 1; sp <= 16; sp *= 2) {
+      // whole words of scales a split, partial results that fit
+      if (sp > 1 && (kb < 4 * sp || !d.workspace || d.workspace_bytes / 4 / sp < (size_t)d.M * d.N)) break;
+      const float us = estimate(d.M, d.N, kb, d.c_f32 != 0, kCfgs[c], sp);
+      if (us < best) {
+        best = us;
+        cfg = c;
+        splits = sp;
+      }
+    }
+  return launch_gemm_fp8_cfg(d, cfg, splits, s);
 }
 
 }  // namespace layup

@@ -29,6 +29,12 @@ __device__ __forceinline__ void copy_block(const char* src, char* lds) {
   __builtin_amdgcn_global_load_lds(src, LDS_PTR(lds), 16, 0, 0);
 }
 
+// 64 words, 4 bytes per lane.
+template <int>
+__device__ __forceinline__ void copy_words(const char* src, char* lds) {
+  __builtin_amdgcn_global_load_lds(src, LDS_PTR(lds), 4, 0, 0);
+}
+
 // LDS reads are inline assembly with explicit lgkmcnt waits: the compiler
 // cannot tell an LDS read apart from the direct-to-LDS copies in flight into
 // other stages.  Offsets are immediates.
@@ -40,6 +46,14 @@ __device__ __forceinline__ u32x4 lds_read_b128(uint32_t a) {
   return v;
 }
 
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read_b32(uint32_t a) {
+  static_assert(OFF >= 0 && OFF < 65536, "LDS immediate offset");
+  uint32_t v;
+  asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
+  return v;
+}
+
 // Wait until at most N LDS reads are outstanding (LDS reads return in order).
 template <int N>
 __device__ __forceinline__ void lgkm_wait() {
@@ -48,6 +62,7 @@ __device__ __forceinline__ void lgkm_wait() {
 
 // Make the MFMA that consumes v depend on the preceding wait.
 __device__ __forceinline__ void after_wait(u32x4& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void after_wait(uint32_t& v) { asm volatile("" : "+v"(v)); }
 
 // s_waitcnt vmcnt(n), expcnt and lgkmcnt left alone (gfx9 encoding).
 #define WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4) | (15 << 8))

@@ -473,6 +473,14 @@ def test_product_tiles(tile, M, N, K, splits, out):
             cfg=TILES[tile], splits=splits)
 
 
+@pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 31, 32])
+@pytest.mark.parametrize("N,K", [(1, 1), (33, 128), (100, 500), (64, 640), (257, 2048), (96, 9000)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_product_of_few_rows(M, N, K, out):
+    """The form for up to 32 rows: partial groups of scale blocks, one to many waves, several groups a wave."""
+    product(M, N, K, "e5m2" if M == 2 else "e4m3", "e4m3", 128 if M == 31 else 1, 128, out=out, pad=N % 2, cfg=4)
+
+
 def test_product_tile_refuses_too_small_a_workspace():
     with pytest.raises(LU.LayupError):
         product(64, 64, 1024, ws=64 * 64 * 4, cfg=3, splits=2)
