@@ -1,6 +1,6 @@
 // C ABI of the calls on the way into a linear layer: dropout, LayerNorm with
 // its residual add, 8-bit quantisation and product.  Argument checks; the
-// kernels are in norm.hip and gemm_fp8.hip.
+// kernels are in norm_fwd.hip, norm_bwd.hip, quant_fp8.hip and gemm_fp8.hip.
 #include <exception>
 
 #include "layup_internal.h"

@@ -22,8 +22,24 @@ __global__ __launch_bounds__(256) void quant_kernel(const QuantArgs P) {
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4, w = threadIdx.x >> 6;
   const int64_t r0 = (int64_t)blockIdx.y * 128 + 8 * rg, c0 = (int64_t)blockIdx.x * 128 + 8 * cg;
   Raw8<T> raw[8];
+  const int64_t n = P.cols - c0;
+  if (r0 + 8 <= P.rows && n >= 8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load_group(raw[i], (const T*)P.x + (r0 + i) * P.ldx + c0, r0 + i < P.rows ? P.cols - c0 : 0);
+    for (int i = 0; i < 8; ++i) raw[i].load((const T*)P.x + (r0 + i) * P.ldx + c0);
+  } else if (r0 < P.rows && n > 0) {
+    // the edge: rows past the last are loaded from it and zeroed
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const T* row = (const T*)P.x + min(r0 + i, P.rows - 1) * P.ldx;
+      load_group(raw[i], row, c0, P.cols);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (r0 + i >= P.rows) raw[i].zero();
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i].zero();
+  }
   uint32_t rmax[8], cmax[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = 0;
@@ -49,8 +65,7 @@ __global__ __launch_bounds__(256) void quant_kernel(const QuantArgs P) {
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) rmax[i] = max(rmax[i], (uint32_t)__shfl_xor((int)rmax[i], o, 64));
+      rmax[i] = lanes16_max(rmax[i]);
 #pragma unroll
       for (int o = 32; o > 8; o >>= 1) cmax[i] = max(cmax[i], (uint32_t)__shfl_xor((int)cmax[i], o, 64));
     }
