@@ -188,6 +188,19 @@ layup_status layup_synchronize(layup_ctx* ctx);
  * changes params outside the library).  Enqueued on the compute stream. */
 layup_status layup_refresh_shadow(layup_ctx* ctx);
 
+/* Dropout of the GPT model's training steps, from the next forward on: the
+ * embeddings' sum and the output of each block's attention and MLP, before it
+ * is added to the residual, are dropped with probability p (GPT-2's embedding
+ * and residual dropout; the attention probabilities are not dropped).  Masks
+ * are layup_dropout_mask's of the [batch*seq, d_model] matrix, with this seed
+ * and offset = step * (2 n_layer + 1) + site, where step counts the context's
+ * completed steps and site is 0 for the embeddings, 1 + 2l and 2 + 2l for
+ * block l's attention and MLP: a step repeated from the same state draws the
+ * same masks, and the backward draws the forward's.  p = 0 (the initial state)
+ * turns dropout off.  0 <= p < 1.  LAYUP_ERR_STATE between a forward and the
+ * end of its backward; LAYUP_ERR_DTYPE for the MLP. */
+layup_status layup_set_dropout(layup_ctx* ctx, float p, uint64_t seed);
+
 /* Forward pass and loss (Algorithm 1 "Forward pass"), followed by the
  * gradient of the mean loss with respect to the logits.
  *   GPT: tokens device int32 [batch, seq+1]; inputs are tokens[:, :seq],

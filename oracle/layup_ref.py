@@ -379,9 +379,15 @@ def _unheads(x: Array) -> Array:
     return x.transpose(0, 2, 1, 3).reshape(b * t, h * dh)
 
 
-def gpt_forward(params, tokens, n_head: int, rnd: Callable = bf16):
+def _dropped(x: Array, keep, site: int) -> Array:
+    return x if keep is None else x * keep[site]
+
+
+def gpt_forward(params, tokens, n_head: int, rnd: Callable = bf16, keep=None):
     """GPT-2 forward (nanoGPT structure, tied head, GELU-tanh, LN eps 1e-5).
-    Returns (loss, dlogits, cache).  bf16 storage points (``rnd``): the
+    Returns (loss, dlogits, cache).  ``keep``: what dropout multiplies each
+    site's [batch*seq, d] matrix by (0 or the factor of kept elements): 0 the
+    embeddings, 1 + 2l and 2 + 2l block l's attention and MLP outputs.  bf16 storage points (``rnd``): the
     weight copies used by the GEMMs, every LayerNorm output, qkv, the
     attention probabilities, the attention output, the MLP pre-activation and
     its GELU, the logits and the logit gradient.  The residual stream, scores
@@ -396,6 +402,7 @@ def gpt_forward(params, tokens, n_head: int, rnd: Callable = bf16):
     n_layer = len([k for k in params if k.endswith(".qkv.w")])
     scale = 1.0 / math.sqrt(dh)
     x = wte[idx] + np.asarray(params["wpe"], np.float64)[np.tile(np.arange(t), bsz)]
+    x = _dropped(x, keep, 0)
     cache = {"idx": idx, "tgt": tgt, "B": bsz, "T": t, "d": d, "H": n_head, "L": n_layer,
              "xs": [x]}
     for l in range(n_layer):
@@ -411,13 +418,13 @@ def gpt_forward(params, tokens, n_head: int, rnd: Callable = bf16):
         c["P"] = P = rnd(causal_softmax(s))
         c["lse"] = causal_logsumexp(s)
         c["o"] = o = rnd(_unheads(P @ v))
-        h_res = x + linear_fwd(o, rnd(params[p + "proj.w"]), params[p + "proj.b"])
+        h_res = x + _dropped(linear_fwd(o, rnd(params[p + "proj.w"]), params[p + "proj.b"]), keep, 1 + 2 * l)
         c["h"] = h_res
         c["a2"] = a2 = rnd(layernorm_fwd(h_res, params[p + "ln2.g"], params[p + "ln2.b"]))
         f = linear_fwd(a2, rnd(params[p + "fc.w"]), params[p + "fc.b"])
         c["f"] = rnd(f)
         c["gl"] = gl = rnd(gelu_tanh(f))
-        x = h_res + linear_fwd(gl, rnd(params[p + "mproj.w"]), params[p + "mproj.b"])
+        x = h_res + _dropped(linear_fwd(gl, rnd(params[p + "mproj.w"]), params[p + "mproj.b"]), keep, 2 + 2 * l)
         cache[l] = c
         cache["xs"].append(x)
     cache["xL"] = x
@@ -428,7 +435,7 @@ def gpt_forward(params, tokens, n_head: int, rnd: Callable = bf16):
     return loss, dlog, cache
 
 
-def gpt_block_bwd(params, c, dx, l, bsz, t, n_head, rnd: Callable = bf16):
+def gpt_block_bwd(params, c, dx, l, bsz, t, n_head, rnd: Callable = bf16, keep=None):
     """Backward of decoder block l given the gradient dx of its output
     (high precision).  Returns (grads of the block's tensors, dx of its
     input)."""
@@ -438,14 +445,14 @@ def gpt_block_bwd(params, c, dx, l, bsz, t, n_head, rnd: Callable = bf16):
     scale = 1.0 / math.sqrt(dh)
     g: Dict[str, Array] = {}
     # MLP output projection; the residual passes dx through unchanged.
-    dy = rnd(dx)
+    dy = rnd(_dropped(dx, keep, 2 + 2 * l))
     g[p + "mproj.w"], g[p + "mproj.b"], dgl = linear_bwd(dy, c["gl"], rnd(params[p + "mproj.w"]))
     df = rnd(dgl * gelu_tanh_grad(c["f"]))
     g[p + "fc.w"], g[p + "fc.b"], da2 = linear_bwd(df, c["a2"], rnd(params[p + "fc.w"]))
     dln2, g[p + "ln2.g"], g[p + "ln2.b"] = layernorm_bwd(da2, c["h"], params[p + "ln2.g"])
     dh_res = dx + dln2
     # attention output projection
-    dy2 = rnd(dh_res)
+    dy2 = rnd(_dropped(dh_res, keep, 1 + 2 * l))
     g[p + "proj.w"], g[p + "proj.b"], do = linear_bwd(dy2, c["o"], rnd(params[p + "proj.w"]))
     do = rnd(do)
     qkv, P = c["qkv"], c["P"]
@@ -477,25 +484,25 @@ def gpt_head_bwd(params, dlog, xf, xL, rnd: Callable = bf16):
     return {"lnf.g": dg, "lnf.b": db}, dx, wte_head
 
 
-def gpt_embed_bwd(dx, idx, wte_head, bsz, t):
+def gpt_embed_bwd(dx, idx, wte_head, bsz, t, keep=None):
     """Backward of the input embeddings x0 = wte[tok] + wpe[pos]: wte
     collects the head's gradient plus dx scattered over the input tokens;
     wpe sums dx over the batch per position."""
-    dx = np.asarray(dx, np.float64)
+    dx = _dropped(np.asarray(dx, np.float64), keep, 0)
     dwte = np.asarray(wte_head, np.float64).copy()
     np.add.at(dwte, np.asarray(idx), dx)
     return {"wte": dwte, "wpe": dx.reshape(bsz, t, -1).sum(axis=0)}
 
 
 def gpt_step(params, m, v, peer, tokens, n_head, hp, alpha, t=1, rnd: Callable = bf16,
-             update: bool = True, store: Callable = f32, push: bool = False):
-    """One layer-wise LayUp step of a GPT stack.  ``params``, ``m``, ``v`` are
+             update: bool = True, store: Callable = f32, push: bool = False, keep=None):
+    """One layer-wise LayUp step of a GPT stack (``keep``: as gpt_forward).  ``params``, ``m``, ``v`` are
     dicts of arrays updated in place (float32 values).  Returns (loss, grads,
     trace, disagreements).  With ``update=False`` only the gradients are
     produced (all units use the pre-step weights either way: a unit's update
     happens after its own backward, and no earlier unit's backward reads it)."""
     params_f = {k_: np.asarray(a_, np.float64) for k_, a_ in params.items()}
-    loss, dlog, cache = gpt_forward(params_f, tokens, n_head, rnd)
+    loss, dlog, cache = gpt_forward(params_f, tokens, n_head, rnd, keep)
     bsz, t_len, n_layer = cache["B"], cache["T"], cache["L"]
     units = gpt_units(n_layer)
     decay = {n for n in params if params[n].ndim >= 2}
@@ -515,12 +522,12 @@ def gpt_step(params, m, v, peer, tokens, n_head, hp, alpha, t=1, rnd: Callable =
         grads[k_] = store(a_)
     apply(n_layer + 1)
     for l in range(n_layer - 1, -1, -1):
-        g, dx = gpt_block_bwd(params_f, cache[l], dx, l, bsz, t_len, n_head, rnd)
+        g, dx = gpt_block_bwd(params_f, cache[l], dx, l, bsz, t_len, n_head, rnd, keep)
         for k_, a_ in g.items():
             grads[k_] = store(a_)
         apply(l + 1)
     # unit 0: embeddings
-    g = gpt_embed_bwd(dx, cache["idx"], wte_head, bsz, t_len)
+    g = gpt_embed_bwd(dx, cache["idx"], wte_head, bsz, t_len, keep)
     for k_, a_ in g.items():
         grads[k_] = store(a_)
     apply(0)

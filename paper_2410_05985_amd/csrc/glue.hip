@@ -443,8 +443,7 @@ int64_t layernorm_bwd_partial_floats(int64_t rows, int d) { return cdiv(rows, LN
 
 hipError_t launch_layernorm_bwd(const float* dy, const float* x, const float* mean,
                                 const float* rstd, const float* g, const float* dres, float* dx,
-                                bf16_t* dx16, float* part, float* dg, float* db, int64_t rows, int d,
-                                hipStream_t s) {
+                                bf16_t* dx16, float* part, int64_t rows, int d, hipStream_t s) {
   if (d % 4 != 0 || d > 256 * 8 || rows <= 0) return hipErrorInvalidValue;
   const unsigned nb = (unsigned)cdiv(rows, LN_ROWS);
   const int nvl = (int)cdiv(d / 4, 64);
@@ -454,8 +453,11 @@ hipError_t launch_layernorm_bwd(const float* dy, const float* x, const float* me
   else if (nvl == 3) e = ln_bwd_launch<3>(dy, x, mean, rstd, g, dres, dx, dx16, part, rows, d, nb, s);
   else if (nvl == 4) e = ln_bwd_launch<4>(dy, x, mean, rstd, g, dres, dx, dx16, part, rows, d, nb, s);
   else e = ln_bwd_launch<8>(dy, x, mean, rstd, g, dres, dx, dx16, part, rows, d, nb, s);
-  if (e != hipSuccess || !dg) return e;
-  ln_partial_sum_kernel<<<(unsigned)ln_sum_teams(d), LN_SUM_THREADS, 0, s>>>(layernorm_sum(part, dg, db, rows, d));
+  return e;
+}
+
+hipError_t launch_layernorm_sum(const LnSum& sum, hipStream_t s) {
+  ln_partial_sum_kernel<<<(unsigned)ln_sum_teams(sum.d), LN_SUM_THREADS, 0, s>>>(sum);
   return hipGetLastError();
 }
 

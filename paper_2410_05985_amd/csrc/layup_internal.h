@@ -226,15 +226,16 @@ hipError_t launch_layernorm_fwd(const float* x, const float* g, const float* b, 
                                 float* mean, float* rstd, int64_t rows, int d, hipStream_t s);
 // LayerNorm backward: dx (float32) and optionally its bfloat16 copy dx16;
 // per-block partial sums of dg and db go to part
-// (layernorm_bwd_partial_floats(rows, d) floats) and are summed into dg, db
-// by a second launch, or, with dg null, by the caller (layernorm_sum).
+// (layernorm_bwd_partial_floats(rows, d) floats), to be summed as
+// layernorm_sum(...) by launch_layernorm_sum or the caller's own launch.
 // d a multiple of 4, at most 2048.
 struct LnSum;
 LnSum layernorm_sum(const float* part, float* dg, float* db, int64_t rows, int d);
+hipError_t launch_layernorm_sum(const LnSum& sum, hipStream_t s);
 int64_t layernorm_bwd_partial_floats(int64_t rows, int d);
 hipError_t launch_layernorm_bwd(const float* dy, const float* x, const float* mean,
                                 const float* rstd, const float* g, const float* dres,
-                                float* dx, bf16_t* dx16, float* part, float* dg, float* db,
+                                float* dx, bf16_t* dx16, float* part,
                                 int64_t rows, int d, hipStream_t s);
 hipError_t launch_softmax_fwd(const float* S, bf16_t* P, int64_t n_mat, int T, float scale,
                               hipStream_t s);
@@ -279,8 +280,12 @@ Mask make_mask(const layup_dropout_mask& d);
 hipError_t launch_dropout(const layup_dropout_desc& d, const Mask& k, hipStream_t s);
 constexpr int NORM_MAX_D = 16384;
 hipError_t launch_norm_fwd(const layup_layernorm_desc& d, const Mask& k, hipStream_t s);
-// dgamma, dbeta: with part (norm_partial_floats floats) and then a second launch
+// Backward with the sums of dgamma and dbeta (a second launch), or its rows
+// alone: part (nullable) then holds norm_partial_rows rows of 2 d floats, to be
+// summed as an LnSum.
 hipError_t launch_norm_bwd(const layup_layernorm_grad_desc& d, const Mask& k, hipStream_t s);
+hipError_t launch_norm_bwd_rows(const layup_layernorm_grad_desc& d, const Mask& k, float* part, hipStream_t s);
+int64_t norm_partial_rows(int64_t rows, int d);
 int64_t norm_partial_floats(int64_t rows, int d);
 hipError_t launch_quant_fp8(const layup_quant_desc& d, hipStream_t s);
 hipError_t launch_gemm_fp8(const layup_gemm_fp8_desc& d, hipStream_t s);

@@ -181,6 +181,10 @@ struct layup_ctx {
   int next_backward = -1;
   std::vector<char> backward_done;
   int32_t step_index = 0;  // value written to the trace
+  // dropout (layup_set_dropout), and as the forward in flight took it
+  float drop_p = 0.f;
+  uint64_t drop_seed = 0, drop_first = 0;  // drop_first: offset of the step's site 0
+  bool drop_on = false;
   bool dx_valid = false;   // dx[cur_dx] holds the input gradient of the last backwarded unit
   // workspace
   size_t ws_bytes = 0;
@@ -283,7 +287,7 @@ size_t carve(layup_ctx* c, char* base) {
     }
     c->do16 = cv.take<bf16_t>(N * d);
     for (auto& q : c->ln_part)
-      for (auto& x : q) x = cv.take<float>(layernorm_bwd_partial_floats(N, (int)d));
+      for (auto& x : q) x = cv.take<float>(std::max(layernorm_bwd_partial_floats(N, (int)d), norm_partial_floats(N, (int)d)));
     c->splitk = cv.take<float>(SPLITK_BYTES / 4);
     c->splitk_bytes = SPLITK_BYTES;
     c->splitk_su = cv.take<float>(SPLITK_SU_BYTES / 4);
@@ -431,6 +435,75 @@ layup_status run_gemm_group(layup_ctx* c, Gemm* g, int n, const LnSum* ln, int n
 }
 
 // ---------------------------------------------------------------- GPT
+// Dropout sites: 0 the embeddings, then each block's attention and MLP.
+int64_t attention_site(int l) { return 1 + 2 * l; }
+int64_t mlp_site(int l) { return 2 + 2 * l; }
+
+Mask site_mask(const layup_ctx* c, int64_t site) {
+  layup_dropout_mask m{};
+  m.p = c->drop_p;
+  m.seed = c->drop_seed;
+  m.offset = c->drop_first + (uint64_t)site;
+  return make_mask(m);
+}
+
+// The residual add and dropout in front of a LayerNorm and the LayerNorm, in
+// one pass: s = residual + dropout(branch), in place of the branch (each thread
+// reads its elements before it writes them).
+hipError_t residual_norm(layup_ctx* c, float* branch, const float* residual, int64_t site, const float* g, const float* b,
+                         bf16_t* y, float* mean, float* rstd) {
+  layup_layernorm_desc n{};
+  n.rows = (int64_t)c->cfg.batch * c->cfg.seq;
+  n.d = c->cfg.d_model;
+  n.eps = 1e-5f;
+  n.x = n.sum = branch;
+  n.residual = residual;
+  n.y = y;
+  n.ldx = n.ldr = n.lds = n.ldy = n.d;
+  n.gamma = g;
+  n.beta = b;
+  n.mean = mean;
+  n.rstd = rstd;
+  n.x_dtype = n.s_dtype = LAYUP_F32;
+  n.y_dtype = LAYUP_BF16;
+  return launch_norm_fwd(n, site_mask(c, site), c->sc);
+}
+
+// Backward of a LayerNorm: dx (float32) = dres + the LayerNorm's part, dy16
+// (nullable) its bfloat16 copy, dropped as the branch of `site` was; partial
+// rows of the weights' gradients in part.
+hipError_t norm_backward(layup_ctx* c, const float* dy, const float* s, const float* mean, const float* rstd,
+                         const float* g, const float* dres, float* dx, bf16_t* dy16, int64_t site, float* part) {
+  const int64_t N = (int64_t)c->cfg.batch * c->cfg.seq;
+  const int d = c->cfg.d_model;
+  if (!c->drop_on)
+    return launch_layernorm_bwd(dy, s, mean, rstd, g, dres, dx, dy16, part, N, d, c->sc);
+  layup_layernorm_grad_desc n{};
+  n.rows = N;
+  n.d = d;
+  n.dy_dtype = n.s_dtype = LAYUP_F32;
+  n.dx_dtype = LAYUP_BF16;
+  n.dy = dy;
+  n.s = s;
+  n.dsum = dres;
+  n.mean = mean;
+  n.rstd = rstd;
+  n.gamma = g;
+  n.dres = dx;
+  n.dx = dy16;
+  n.lddy = n.lds = n.lddsum = n.lddres = n.lddx = d;
+  return launch_norm_bwd_rows(n, site_mask(c, site), part, c->sc);
+}
+
+// The sum of those partial rows.
+LnSum norm_sums(const layup_ctx* c, const float* part, float* dg, float* db) {
+  const int64_t N = (int64_t)c->cfg.batch * c->cfg.seq;
+  const int d = c->cfg.d_model;
+  LnSum sum = layernorm_sum(part, dg, db, N, d);
+  if (c->drop_on) sum.nb = norm_partial_rows(N, d);
+  return sum;
+}
+
 layup_status gpt_forward(layup_ctx* c, const int32_t* tokens, float* loss_out) {
   const layup_config& g = c->cfg;
   const hipStream_t s = c->sc;
@@ -442,14 +515,21 @@ layup_status gpt_forward(layup_ctx* c, const int32_t* tokens, float* loss_out) {
   // two streams were slower: 12.00 against 11.65 ms a GPT-2-small step,
   // 13.38 against 12.77 ms at the 1.3B stack's width -- half-size products
   // waste more than the overlap hides.)
+  // With dropout the products of a branch write it by itself, and the residual
+  // add and the dropout go with the LayerNorm behind it.
+  const bool drop = c->drop_on;
   HIPCHK(c, launch_embed_fwd(tokens, fl.p("wte"), fl.p("wpe"), c->acts[0].x, (int)B, (int)T, (int)d, g.vocab, s),
          "embedding");
   for (int l = 0; l < g.n_layer; ++l) {
     BlockActs& A = c->acts[l];
     const std::string p = "h" + std::to_string(l) + ".";
     float* x_next = (l + 1 < g.n_layer) ? c->acts[l + 1].x : c->xL;
-    HIPCHK(c, launch_layernorm_fwd(A.x, fl.p(p + "ln1.g"), fl.p(p + "ln1.b"), A.a, A.mean1, A.rstd1, N, (int)d, s),
-           "ln1");
+    if (drop)
+      HIPCHK(c, residual_norm(c, A.x, l ? c->acts[l - 1].h : nullptr, l ? mlp_site(l - 1) : 0, fl.p(p + "ln1.g"),
+                              fl.p(p + "ln1.b"), A.a, A.mean1, A.rstd1), "dropout + ln1");
+    else
+      HIPCHK(c, launch_layernorm_fwd(A.x, fl.p(p + "ln1.g"), fl.p(p + "ln1.b"), A.a, A.mean1, A.rstd1, N, (int)d, s),
+             "ln1");
     Gemm q = mk(true, true, N, 3 * d, d, A.a, d, fl.w16(p + "qkv.w"), d, A.qkv, 3 * d, EPI_BF16);
     q.bias = fl.p(p + "qkv.b");
     TRY(run_gemm(c, q, "qkv forward"));
@@ -483,20 +563,28 @@ layup_status gpt_forward(layup_ctx* c, const int32_t* tokens, float* loss_out) {
     }
     Gemm pr = mk(true, true, N, d, d, A.o, d, fl.w16(p + "proj.w"), d, A.h, d, EPI_F32);
     pr.bias = fl.p(p + "proj.b");
-    pr.aux = A.x;
+    if (!drop) pr.aux = A.x;
     TRY(run_gemm(c, pr, "proj forward"));
-    HIPCHK(c, launch_layernorm_fwd(A.h, fl.p(p + "ln2.g"), fl.p(p + "ln2.b"), A.a2, A.mean2, A.rstd2, N, (int)d, s),
-           "ln2");
+    if (drop)
+      HIPCHK(c, residual_norm(c, A.h, A.x, attention_site(l), fl.p(p + "ln2.g"), fl.p(p + "ln2.b"), A.a2, A.mean2,
+                              A.rstd2), "dropout + ln2");
+    else
+      HIPCHK(c, launch_layernorm_fwd(A.h, fl.p(p + "ln2.g"), fl.p(p + "ln2.b"), A.a2, A.mean2, A.rstd2, N, (int)d, s),
+             "ln2");
     Gemm fc = mk(true, true, N, F, d, A.a2, d, fl.w16(p + "fc.w"), d, A.f, F, EPI_GELU);
     fc.bias = fl.p(p + "fc.b");
     fc.C2 = A.gl;
     TRY(run_gemm(c, fc, "fc forward"));
     Gemm mp = mk(true, true, N, d, F, A.gl, F, fl.w16(p + "mproj.w"), F, x_next, d, EPI_F32);
     mp.bias = fl.p(p + "mproj.b");
-    mp.aux = A.h;
+    if (!drop) mp.aux = A.h;
     TRY(run_gemm(c, mp, "mproj forward"));
   }
-  HIPCHK(c, launch_layernorm_fwd(c->xL, fl.p("lnf.g"), fl.p("lnf.b"), c->xf, c->meanf, c->rstdf, N, (int)d, s), "lnf");
+  if (drop)
+    HIPCHK(c, residual_norm(c, c->xL, c->acts[g.n_layer - 1].h, mlp_site(g.n_layer - 1), fl.p("lnf.g"), fl.p("lnf.b"),
+                            c->xf, c->meanf, c->rstdf), "dropout + lnf");
+  else
+    HIPCHK(c, launch_layernorm_fwd(c->xL, fl.p("lnf.g"), fl.p("lnf.b"), c->xf, c->meanf, c->rstdf, N, (int)d, s), "lnf");
   TRY(run_gemm(c, mk(true, true, N, Vp, d, c->xf, d, fl.w16("wte"), d, c->logits, Vp, EPI_BF16), "head forward"));
   HIPCHK(c, launch_ce_fwd_bwd(c->logits, Vp, tokens, (int)B, (int)T, g.vocab, c->logits, c->loss_rows, loss_out, s),
          "cross-entropy");
@@ -525,13 +613,22 @@ layup_status gpt_backward(layup_ctx* c, int u) {
     // the tied wte's gradient: the embedding backward adds the tokens' rows at the end
     TRY(run_gemm(c, mk(false, false, Vp, d, N, c->logits, Vp, c->xf, d, fl.g("wte"), d, EPI_F32), "head dW"));
     c->cur_dx = 0;
-    HIPCHK(c, launch_layernorm_bwd(c->da, c->xL, c->meanf, c->rstdf, fl.p("lnf.g"), nullptr,
-                                   c->dx[0], c->dyA[(g.n_layer - 1) & 1], c->ln_part[g.n_layer & 1][0],
-                                   fl.g("lnf.g"), fl.g("lnf.b"), N, (int)d, s), "lnf backward");
+    float* const part = c->ln_part[g.n_layer & 1][0];
+    HIPCHK(c, norm_backward(c, c->da, c->xL, c->meanf, c->rstdf, fl.p("lnf.g"), nullptr, c->dx[0],
+                            c->dyA[(g.n_layer - 1) & 1], mlp_site(g.n_layer - 1), part), "lnf backward");
+    HIPCHK(c, launch_layernorm_sum(norm_sums(c, part, fl.g("lnf.g"), fl.g("lnf.b")), s), "lnf gradient sums");
     return LAYUP_OK;
   }
   if (u == 0) {
     if (c->su != s) HIPCHK(c, hipStreamWaitEvent(s, c->ev_sort, 0), "wait token sort");
+    if (c->drop_on) {  // the embeddings' dropout
+      layup_dropout_desc m{};
+      m.rows = N;
+      m.cols = m.ldx = m.ldy = d;
+      m.x = m.y = c->dx[c->cur_dx];
+      m.dtype = LAYUP_F32;
+      HIPCHK(c, launch_dropout(m, site_mask(c, 0), s), "embedding dropout backward");
+    }
     HIPCHK(c, launch_embed_bwd(c->dx[c->cur_dx], (const int32_t*)c->sorted, fl.g("wte"), fl.g("wpe"),
                                (int)B, (int)T, (int)d, g.vocab, s), "embedding backward");
     return LAYUP_OK;
@@ -556,8 +653,8 @@ layup_status gpt_backward(layup_ctx* c, int u) {
   TRY(run_gemm(c, dg, "mproj dX + gelu backward", true));
   // MLP input projection: dY = df16
   TRY(run_gemm(c, mk(true, false, N, d, F, df16, F, fl.w16(p + "fc.w"), d, c->da, d, EPI_F32), "fc dX", true));
-  HIPCHK(c, launch_layernorm_bwd(c->da, A.h, A.mean2, A.rstd2, fl.p(p + "ln2.g"), dxo, c->dh,
-                                 dyB, c->ln_part[pq][1], nullptr, nullptr, N, (int)d, s), "ln2 backward");
+  HIPCHK(c, norm_backward(c, c->da, A.h, A.mean2, A.rstd2, fl.p(p + "ln2.g"), dxo, c->dh, dyB, attention_site(l),
+                          c->ln_part[pq][1]), "ln2 backward");
   // attention output projection: dY = dyB = bf16(dh) from the LayerNorm backward above
   TRY(run_gemm(c, mk(true, false, N, d, d, dyB, d, fl.w16(p + "proj.w"), d, c->do16, d, EPI_BF16), "proj dX", true));
   if (A.of) {
@@ -606,16 +703,15 @@ layup_status gpt_backward(layup_ctx* c, int u) {
                  dw(F, d, df16, A.a2, "fc.w", "fc.b"), dw(d, F, dyA, A.gl, "mproj.w", "mproj.b")};
   // the LayerNorms' gradient sums ride along (a launch of their own each took
   // 5 us, 24 a GPT-2-small step)
-  const LnSum sums[2] = {layernorm_sum(c->ln_part[pq][0], fl.g(p + "ln1.g"), fl.g(p + "ln1.b"), N, (int)d),
-                         layernorm_sum(c->ln_part[pq][1], fl.g(p + "ln2.g"), fl.g(p + "ln2.b"), N, (int)d)};
+  const LnSum sums[2] = {norm_sums(c, c->ln_part[pq][0], fl.g(p + "ln1.g"), fl.g(p + "ln1.b")),
+                         norm_sums(c, c->ln_part[pq][1], fl.g(p + "ln2.g"), fl.g(p + "ln2.b"))};
   // the next block's operands (and partial rows) were last read by the dW
   // launch of the block before this one; one wait a block covers them all
   // (its unit's event follows it on the update stream)
   if (side && l + 1 < (int)g.n_layer) HIPCHK(c, hipStreamWaitEvent(s, c->ev_unit[u + 1], 0), "wait operands free");
   // LayerNorm 1; its bf16 dx is the next block's output-gradient operand
-  HIPCHK(c, launch_layernorm_bwd(c->da, A.x, A.mean1, A.rstd1, fl.p(p + "ln1.g"), c->dh, dxi,
-                                 l > 0 ? c->dyA[pq ^ 1] : nullptr, c->ln_part[pq][0], nullptr, nullptr, N, (int)d, s),
-         "ln1 backward");
+  HIPCHK(c, norm_backward(c, c->da, A.x, A.mean1, A.rstd1, fl.p(p + "ln1.g"), c->dh, dxi, l > 0 ? c->dyA[pq ^ 1] : nullptr,
+                          l > 0 ? mlp_site(l - 1) : 0, c->ln_part[pq][0]), "ln1 backward");
   if (side) {
     HIPCHK(c, hipEventRecord(c->ev_unit[u], s), "record unit event");
     HIPCHK(c, hipStreamWaitEvent(c->su, c->ev_unit[u], 0), "wait unit event");
@@ -1021,12 +1117,24 @@ layup_status layup_forward(layup_ctx* ctx, const int32_t* tokens, const float* x
   ctx->timeline_valid = false;
   ctx->dx_valid = false;
   ctx->tokens = tokens;
+  ctx->drop_on = site_mask(ctx, 0).thr != 0;
+  ctx->drop_first = (uint64_t)ctx->step_index * (uint64_t)(2 * ctx->cfg.n_layer + 1);
   layup_status st = ctx->cfg.model == LAYUP_MODEL_GPT_BF16 ? gpt_forward(ctx, tokens, loss_out)
                                                             : mlp_forward(ctx, tokens, x, loss_out);
   if (st != LAYUP_OK) return st;
   HIPCHK(ctx, hipEventRecord(ctx->ev_fwd_end, ctx->sc), "record forward end");
   ctx->forward_done = true;
   ctx->next_backward = ctx->L.n_units - 1;
+  return LAYUP_OK;
+}
+
+layup_status layup_set_dropout(layup_ctx* ctx, float p, uint64_t seed) {
+  if (!ctx) return fail(nullptr, LAYUP_ERR_INVALID_ARG, "null context");
+  if (ctx->cfg.model != LAYUP_MODEL_GPT_BF16) return fail(ctx, LAYUP_ERR_DTYPE, "dropout is for the GPT model");
+  if (!(p >= 0.f && p < 1.f)) return fail(ctx, LAYUP_ERR_INVALID_ARG, "dropout probability must be at least 0 and below 1");
+  if (ctx->forward_done) return fail(ctx, LAYUP_ERR_STATE, "dropout changed between a forward and its backward");
+  ctx->drop_p = p;
+  ctx->drop_seed = seed;
   return LAYUP_OK;
 }
 

@@ -164,6 +164,7 @@ static int64_t bwd_blocks(int64_t rows, int d) {
   return std::min<int64_t>(cdiv(rows, rpb), 512);
 }
 
+int64_t norm_partial_rows(int64_t rows, int d) { return bwd_blocks(rows, d); }
 int64_t norm_partial_floats(int64_t rows, int d) { return bwd_blocks(rows, d) * 2 * (int64_t)d; }
 
 template <class TY, class TS, class TX, int TPR, int NV, bool WHOLE>
@@ -204,21 +205,23 @@ static hipError_t bwd_type(const BwdArgs& P, bool xf, hipStream_t s) {
   return xf ? bwd_width<TY, TS, float>(P, s) : bwd_width<TY, TS, bf16_t>(P, s);
 }
 
+hipError_t launch_norm_bwd_rows(const layup_layernorm_grad_desc& d, const Mask& k, float* part, hipStream_t s) {
+  const BwdArgs P{d.dy,   d.s,   d.dsum,   d.dres,   d.dx,   d.mean, d.rstd, d.gamma, part,
+                  d.lddy, d.lds, d.lddsum, d.lddres, d.lddx, d.rows, d.d,    k};
+  const bool yf = d.dy_dtype == LAYUP_F32, sf = d.s_dtype == LAYUP_F32, xf = d.dx_dtype == LAYUP_F32;
+  if (yf) return sf ? bwd_type<float, float>(P, xf, s) : bwd_type<float, bf16_t>(P, xf, s);
+  return sf ? bwd_type<bf16_t, float>(P, xf, s) : bwd_type<bf16_t, bf16_t>(P, xf, s);
+}
+
 hipError_t launch_norm_bwd(const layup_layernorm_grad_desc& d, const Mask& k, hipStream_t s) {
   const bool sums = d.dgamma || d.dbeta;
-  const int64_t nb = bwd_blocks(d.rows, d.d);
   if (d.rows > 0) {
-    const BwdArgs P{d.dy,   d.s,   d.dsum,   d.dres,   d.dx,   d.mean, d.rstd, d.gamma, sums ? (float*)d.workspace : nullptr,
-                    d.lddy, d.lds, d.lddsum, d.lddres, d.lddx, d.rows, d.d,    k};
-    const bool yf = d.dy_dtype == LAYUP_F32, sf = d.s_dtype == LAYUP_F32, xf = d.dx_dtype == LAYUP_F32;
-    hipError_t e;
-    if (yf) e = sf ? bwd_type<float, float>(P, xf, s) : bwd_type<float, bf16_t>(P, xf, s);
-    else e = sf ? bwd_type<bf16_t, float>(P, xf, s) : bwd_type<bf16_t, bf16_t>(P, xf, s);
+    const hipError_t e = launch_norm_bwd_rows(d, k, sums ? (float*)d.workspace : nullptr, s);
     if (e != hipSuccess) return e;
   }
   if (!sums) return hipSuccess;
-  norm_sum_kernel<<<(unsigned)cdiv(2 * d.d, SUM_COLS), SUM_COLS * SUM_LANES, 0, s>>>((const float*)d.workspace, (int)nb, d.d,
-                                                                                     d.dgamma, d.dbeta);
+  norm_sum_kernel<<<(unsigned)cdiv(2 * d.d, SUM_COLS), SUM_COLS * SUM_LANES, 0, s>>>(
+      (const float*)d.workspace, (int)bwd_blocks(d.rows, d.d), d.d, d.dgamma, d.dbeta);
   return hipGetLastError();
 }
 

@@ -131,7 +131,7 @@ class layup_gemm_fp8_desc(C.Structure):
 EXPORTS = [
     "layup_param_layout", "layup_tensor_layout", "layup_workspace_size", "layup_init",
     "layup_destroy", "layup_last_error", "layup_global_error", "layup_synchronize",
-    "layup_refresh_shadow", "layup_forward", "layup_layer_backward", "layup_unit_update_mix",
+    "layup_refresh_shadow", "layup_set_dropout", "layup_forward", "layup_layer_backward", "layup_unit_update_mix",
     "layup_layer_update_mix", "layup_layer_update_mix_static", "layup_units_update_mix",
     "layup_unit_update_push", "layup_step_ex", "layup_step",
     "layup_unit_timeline", "layup_gemm_timing", "layup_gemm_timing_read", "layup_push_sum_send", "layup_push_sum_receive", "layup_activation",
@@ -163,6 +163,7 @@ def lib() -> C.CDLL:
         "layup_global_error": ([], C.c_char_p),
         "layup_synchronize": ([P], C.c_int),
         "layup_refresh_shadow": ([P], C.c_int),
+        "layup_set_dropout": ([P, C.c_float, C.c_uint64], C.c_int),
         "layup_forward": ([P, P, P, P], C.c_int),
         "layup_layer_backward": ([P, C.c_int32], C.c_int),
         "layup_unit_update_mix": ([P, C.c_int32, P, C.c_float, C.c_int32, P], C.c_int),
@@ -296,6 +297,10 @@ def layup_synchronize(ctx):
 
 def layup_refresh_shadow(ctx):
     _check(lib().layup_refresh_shadow(ctx), ctx)
+
+
+def layup_set_dropout(ctx, p: float, seed: int = 0):
+    _check(lib().layup_set_dropout(ctx, p, seed), ctx)
 
 
 def layup_forward(ctx, tokens, x=None, loss_out=None):

@@ -99,3 +99,29 @@ def test_quantise_scales(fmt, block_rows):
                 assert big <= 1.75 * 2.0 ** (top + int(e[i, j]) - 127) and big > 1.75 * 2.0 ** (top + int(e[i, j]) - 128)
             err = np.abs(v[at] - x[at])[fin[at]]
             assert (err <= np.maximum(np.abs(x[at])[fin[at]] * 2.0 ** -(bits + 1), big * 2.0 ** -(bits + 1) * 2.0 ** -13)).all()
+
+
+def test_gpt_step_with_dropout_by_differences():
+    """Every gradient of a tiny two-block GPT with dropout at its sites, against central differences of its loss."""
+    import oracle as O
+    from paper_2410_05985_amd import synthetic as S
+    cfg = S.GPTConfig(n_layer=2, d_model=8, n_head=2, d_ff=16, seq=4, batch=2, vocab=11)
+    rng = np.random.default_rng(6)
+    params = {n: rng.standard_normal(s) * (0.3 if len(s) >= 2 else 0.1) + (1.0 if n.endswith(".g") else 0.0)
+              for n, s, _ in S.gpt_param_specs(cfg)}
+    tokens = rng.integers(0, cfg.vocab, (cfg.batch, cfg.seq + 1))
+    keep = [R.keep_mask(8, 8, 0.4, 3, site) * R.drop_scale(0.4) for site in range(5)]
+    hp = dict(optim="adamw", lr=0.0, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.0)
+    _, grads, _, _ = O.gpt_step({k: v.copy() for k, v in params.items()}, None, None, None, tokens, cfg.n_head, hp, 0.0,
+                                rnd=O.ident, update=False, store=O.ident, keep=keep)
+    loss = lambda: O.gpt_forward(params, tokens, cfg.n_head, rnd=O.ident, keep=keep)[0]  # noqa: E731
+    h = 1e-5
+    for n, a in params.items():
+        for i in list(np.ndindex(*a.shape))[::5]:
+            old = a[i]
+            a[i] = old + h
+            up = loss()
+            a[i] = old - h
+            down = loss()
+            a[i] = old
+            assert (up - down) / (2 * h) == pytest.approx(grads[n][i], rel=1e-5, abs=1e-9), (n, i)
