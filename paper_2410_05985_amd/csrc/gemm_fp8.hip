@@ -609,7 +609,7 @@ struct TileCfg {
   } t[2];
 };
 const TileCfg kCfgs[kNumCfg] = {
-    {256, 256, 1, {{1.01f, 0.73f, 15.0f, 1300.f}, {2.27f, 2.02f, 15.4f, 1800.f}}},  // 2 x 4 waves, 2 stages
+    {256, 256, 1, {{1.01f, 0.73f, 17.0f, 1300.f}, {2.27f, 2.02f, 15.4f, 1800.f}}},  // 2 x 4 waves, 2 stages
     {256, 128, 1, {{0.59f, 0.44f, 7.5f, 1300.f}, {1.27f, 1.15f, 8.0f, 2000.f}}},    // 4 x 2 waves, 3 stages
     {128, 128, 2, {{0.53f, 0.54f, 4.5f, 1220.f}, {0.76f, 1.21f, 5.2f, 1950.f}}},    // 2 x 2 waves, 2 stages
     {64, 64, 4, {{0.37f, 0.55f, 1.6f, 1130.f}, {0.40f, 0.91f, 1.9f, 1970.f}}},      // 2 x 2 waves, 2 stages

@@ -30,6 +30,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(const BwdArgs
     const int c = 8 * (t + TPR * j);
     Raw8<float> rg;
     if (P.gamma) load_group<WHOLE>(rg, P.gamma, c, d);
+    if (P.gamma) finish_group<WHOLE>(rg, P.gamma, c, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       g[j][e] = P.gamma ? rg.get(e) : 1.f;
@@ -47,6 +48,13 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(const BwdArgs
       if (P.dsum) load_group<WHOLE>(rd[j], (const TS*)P.dsum + row * P.lddsum, c, d);
     }
     const float mu = P.mean[row], r = P.rstd[row];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = 8 * (t + TPR * j);
+      finish_group<WHOLE>(ry[j], (const TY*)P.dy + row * P.lddy, c, d);
+      finish_group<WHOLE>(rs[j], (const TS*)P.s + row * P.lds, c, d);
+      if (P.dsum) finish_group<WHOLE>(rd[j], (const TS*)P.dsum + row * P.lddsum, c, d);
+    }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -160,7 +168,7 @@ __global__ __launch_bounds__(SUM_COLS * SUM_LANES) void norm_sum_kernel(const fl
 
 // Blocks of the backward (and partial rows).
 static int64_t bwd_blocks(int64_t rows, int d) {
-  const int tpr = team_of(d), rpb = threads_of(tpr) / tpr;
+  const int tpr = team_of(rows, d), rpb = threads_of(tpr) / tpr;
   return std::min<int64_t>(cdiv(rows, rpb), 512);
 }
 
@@ -174,18 +182,19 @@ static hipError_t bwd_launch(const BwdArgs& P, hipStream_t s) {
 }
 template <class TY, class TS, class TX>
 static hipError_t bwd_width(const BwdArgs& P, hipStream_t s) {
-  const int nv = (int)cdiv(cdiv(P.d, 8), team_of(P.d));
+  const int team = team_of(P.rows, P.d), nv = (int)cdiv(cdiv(P.d, 8), team);
   if (P.d % 8) {  // fewer forms for widths off the groups
-    switch (team_of(P.d)) {
+    switch (team) {
       case 32:
         return nv <= 1 ? bwd_launch<TY, TS, TX, 32, 1, false>(P, s)
                        : nv == 2 ? bwd_launch<TY, TS, TX, 32, 2, false>(P, s) : bwd_launch<TY, TS, TX, 32, 4, false>(P, s);
-      case 64: return nv <= 3 ? bwd_launch<TY, TS, TX, 64, 3, false>(P, s) : bwd_launch<TY, TS, TX, 64, 4, false>(P, s);
-      case 256: return nv <= 2 ? bwd_launch<TY, TS, TX, 256, 2, false>(P, s) : bwd_launch<TY, TS, TX, 256, 4, false>(P, s);
-      default: return bwd_launch<TY, TS, TX, 1024, 2, false>(P, s);
+      case 256:
+        return nv <= 1 ? bwd_launch<TY, TS, TX, 256, 1, false>(P, s)
+                       : nv == 2 ? bwd_launch<TY, TS, TX, 256, 2, false>(P, s) : bwd_launch<TY, TS, TX, 256, 4, false>(P, s);
+      default: return nv <= 1 ? bwd_launch<TY, TS, TX, 1024, 1, false>(P, s) : bwd_launch<TY, TS, TX, 1024, 2, false>(P, s);
     }
   }
-  switch (team_of(P.d)) {
+  switch (team) {
     case 32:
       switch (nv) {
         case 1: return bwd_launch<TY, TS, TX, 32, 1, true>(P, s);
@@ -193,11 +202,14 @@ static hipError_t bwd_width(const BwdArgs& P, hipStream_t s) {
         case 3: return bwd_launch<TY, TS, TX, 32, 3, true>(P, s);
         default: return bwd_launch<TY, TS, TX, 32, 4, true>(P, s);
       }
-    case 64: return nv <= 3 ? bwd_launch<TY, TS, TX, 64, 3, true>(P, s) : bwd_launch<TY, TS, TX, 64, 4, true>(P, s);
     case 256:
-      return nv <= 2 ? bwd_launch<TY, TS, TX, 256, 2, true>(P, s)
-                     : nv == 3 ? bwd_launch<TY, TS, TX, 256, 3, true>(P, s) : bwd_launch<TY, TS, TX, 256, 4, true>(P, s);
-    default: return bwd_launch<TY, TS, TX, 1024, 2, true>(P, s);
+      switch (nv) {
+        case 1: return bwd_launch<TY, TS, TX, 256, 1, true>(P, s);
+        case 2: return bwd_launch<TY, TS, TX, 256, 2, true>(P, s);
+        case 3: return bwd_launch<TY, TS, TX, 256, 3, true>(P, s);
+        default: return bwd_launch<TY, TS, TX, 256, 4, true>(P, s);
+      }
+    default: return nv <= 1 ? bwd_launch<TY, TS, TX, 1024, 1, true>(P, s) : bwd_launch<TY, TS, TX, 1024, 2, true>(P, s);
   }
 }
 template <class TY, class TS>

@@ -28,6 +28,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T
   const int64_t c = (int64_t)g * 8, n = cols - c;
   Raw8<T> r;
   load_group(r, x + (int64_t)row * ldx, c, cols);
+  finish_group(r, x + (int64_t)row * ldx, c, cols);
   float f[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = r.get(e);
@@ -98,6 +99,16 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(const FwdArgs
       if (P.beta) load_group<WHOLE>(rb[j], P.beta, c, d);
     }
   }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = 8 * (t + TPR * j);
+    finish_group<WHOLE>(rx[j], x, c, d);
+    if (P.res) finish_group<WHOLE>(rr[j], res, c, d);
+    if constexpr (EARLY) {
+      if (P.gamma) finish_group<WHOLE>(rg[j], P.gamma, c, d);
+      if (P.beta) finish_group<WHOLE>(rb[j], P.beta, c, d);
+    }
+  }
   const uint64_t offset = mask_offset(P.K);
   float v[NV][8];
   float s = 0.f, ss = 0.f;
@@ -137,6 +148,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(const FwdArgs
     if constexpr (!EARLY) {
       if (P.gamma) load_group<WHOLE>(rg[j], P.gamma, c, d);
       if (P.beta) load_group<WHOLE>(rb[j], P.beta, c, d);
+      if (P.gamma) finish_group<WHOLE>(rg[j], P.gamma, c, d);
+      if (P.beta) finish_group<WHOLE>(rb[j], P.beta, c, d);
     }
     const Raw8<float>&g = rg[j], &b = rb[j];
     float y[8];
@@ -175,18 +188,19 @@ static hipError_t fwd_launch(const FwdArgs& P, hipStream_t s) {
 }
 template <class TX, class TS, int YD>
 static hipError_t fwd_width(const FwdArgs& P, hipStream_t s) {
-  const int nv = (int)cdiv(cdiv(P.d, 8), team_of(P.d));
+  const int team = team_of(P.rows, P.d), nv = (int)cdiv(cdiv(P.d, 8), team);
   if (P.d % 8) {  // fewer forms for widths off the groups
-    switch (team_of(P.d)) {
+    switch (team) {
       case 32:
         return nv <= 1 ? fwd_launch<TX, TS, YD, 32, 1, false>(P, s)
                        : nv == 2 ? fwd_launch<TX, TS, YD, 32, 2, false>(P, s) : fwd_launch<TX, TS, YD, 32, 4, false>(P, s);
-      case 64: return nv <= 3 ? fwd_launch<TX, TS, YD, 64, 3, false>(P, s) : fwd_launch<TX, TS, YD, 64, 4, false>(P, s);
-      case 256: return nv <= 2 ? fwd_launch<TX, TS, YD, 256, 2, false>(P, s) : fwd_launch<TX, TS, YD, 256, 4, false>(P, s);
-      default: return fwd_launch<TX, TS, YD, 1024, 2, false>(P, s);
+      case 256:
+        return nv <= 1 ? fwd_launch<TX, TS, YD, 256, 1, false>(P, s)
+                       : nv == 2 ? fwd_launch<TX, TS, YD, 256, 2, false>(P, s) : fwd_launch<TX, TS, YD, 256, 4, false>(P, s);
+      default: return nv <= 1 ? fwd_launch<TX, TS, YD, 1024, 1, false>(P, s) : fwd_launch<TX, TS, YD, 1024, 2, false>(P, s);
     }
   }
-  switch (team_of(P.d)) {
+  switch (team) {
     case 32:
       switch (nv) {
         case 1: return fwd_launch<TX, TS, YD, 32, 1, true>(P, s);
@@ -194,11 +208,14 @@ static hipError_t fwd_width(const FwdArgs& P, hipStream_t s) {
         case 3: return fwd_launch<TX, TS, YD, 32, 3, true>(P, s);
         default: return fwd_launch<TX, TS, YD, 32, 4, true>(P, s);
       }
-    case 64: return nv <= 3 ? fwd_launch<TX, TS, YD, 64, 3, true>(P, s) : fwd_launch<TX, TS, YD, 64, 4, true>(P, s);
     case 256:
-      return nv <= 2 ? fwd_launch<TX, TS, YD, 256, 2, true>(P, s)
-                     : nv == 3 ? fwd_launch<TX, TS, YD, 256, 3, true>(P, s) : fwd_launch<TX, TS, YD, 256, 4, true>(P, s);
-    default: return fwd_launch<TX, TS, YD, 1024, 2, true>(P, s);
+      switch (nv) {
+        case 1: return fwd_launch<TX, TS, YD, 256, 1, true>(P, s);
+        case 2: return fwd_launch<TX, TS, YD, 256, 2, true>(P, s);
+        case 3: return fwd_launch<TX, TS, YD, 256, 3, true>(P, s);
+        default: return fwd_launch<TX, TS, YD, 256, 4, true>(P, s);
+      }
+    default: return nv <= 1 ? fwd_launch<TX, TS, YD, 1024, 1, true>(P, s) : fwd_launch<TX, TS, YD, 1024, 2, true>(P, s);
   }
 }
 template <class TX, class TS>

@@ -6,45 +6,39 @@ namespace layup {
 
 namespace {
 
-// One block takes a tile of 128 x 128, thread t the columns 8 (t % 16) .. of
-// the rows 8 (t / 16) .. + 7: an 8 x 8 patch, so that both q and qt leave the
-// registers in 8-byte pieces.
+// One block takes a tile of 128 x 128, thread t the columns 8 (t % 16) .. + 7 of
+// R rows from R (t / 16) on.  R = 8 (256 threads): an 8 x 8 patch, so that both
+// q and qt leave the registers in 8-byte pieces.  R = 2 (1024 threads) where
+// there are few tiles, which then wait for their slowest thread.
 struct QuantArgs {
   const void* x;
   uint8_t *q, *scale, *qt, *scale_t;
   int64_t rows, cols, ldx, ldq, ldsc, ldqt, ldsct;
 };
 
-template <class T, int TOP, bool BLOCK>
-__global__ __launch_bounds__(256) void quant_kernel(const QuantArgs P) {
-  __shared__ uint32_t red[4][128];
-  __shared__ uint8_t tile[128][136];
+template <class T, int TOP, bool BLOCK, int R>
+__global__ __launch_bounds__(2048 / R) void quant_kernel(const QuantArgs P) {
+  constexpr int WAVES = 32 / R;
+  __shared__ uint32_t red[WAVES][128];
+  __shared__ __attribute__((aligned(8))) uint8_t tile[128][136];
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4, w = threadIdx.x >> 6;
-  const int64_t r0 = (int64_t)blockIdx.y * 128 + 8 * rg, c0 = (int64_t)blockIdx.x * 128 + 8 * cg;
-  Raw8<T> raw[8];
-  const int64_t n = P.cols - c0;
-  if (r0 + 8 <= P.rows && n >= 8) {
+  const int64_t r0 = (int64_t)blockIdx.y * 128 + R * rg, c0 = (int64_t)blockIdx.x * 128 + 8 * cg;
+  Raw8<T> raw[R];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i].load((const T*)P.x + (r0 + i) * P.ldx + c0);
-  } else if (r0 < P.rows && n > 0) {
-    // the edge: rows past the last are loaded from it and zeroed
+  for (int i = 0; i < R; ++i)  // rows past the last: that again, zeroed below
+    load_group(raw[i], (const T*)P.x + min(r0 + i, P.rows - 1) * P.ldx, c0, P.cols);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const T* row = (const T*)P.x + min(r0 + i, P.rows - 1) * P.ldx;
-      load_group(raw[i], row, c0, P.cols);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (r0 + i >= P.rows) raw[i].zero();
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i].zero();
+  for (int i = 0; i < R; ++i) {
+    finish_group(raw[i], (const T*)P.x + min(r0 + i, P.rows - 1) * P.ldx, c0, P.cols);
+    if (r0 + i >= P.rows) raw[i].zero();
   }
-  uint32_t rmax[8], cmax[8];
+  uint32_t rmax[R], cmax[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = 0;
+  for (int i = 0; i < R; ++i) rmax[i] = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int e = 0; e < 8; ++e) cmax[e] = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t a = finite_bits(raw[i].get(e));
@@ -54,33 +48,45 @@ __global__ __launch_bounds__(256) void quant_kernel(const QuantArgs P) {
   if constexpr (BLOCK) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, rmax[i]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-    if ((threadIdx.x & 63) == 0) red[w][0] = m;
+    for (int i = 0; i < R; ++i) m = max(m, rmax[i]);
+    m = lanes16_max(m);
+    if (cg == 0) red[0][rg] = m;
     __syncthreads();
-    m = max(max(red[0][0], red[1][0]), max(red[2][0], red[3][0]));
+    m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = m;
+    for (int i = 0; i < 128 / R; ++i) m = max(m, red[0][i]);
+#pragma unroll
+    for (int i = 0; i < R; ++i) rmax[i] = m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) cmax[e] = m;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      rmax[i] = lanes16_max(rmax[i]);
+    for (int i = 0; i < R; ++i) rmax[i] = lanes16_max(rmax[i]);
+    if (P.qt) {
 #pragma unroll
-      for (int o = 32; o > 8; o >>= 1) cmax[i] = max(cmax[i], (uint32_t)__shfl_xor((int)cmax[i], o, 64));
+      for (int e = 0; e < 8; ++e) {
+        cmax[e] = max(cmax[e], (uint32_t)__shfl_xor((int)cmax[e], 16, 64));
+        cmax[e] = max(cmax[e], (uint32_t)__shfl_xor((int)cmax[e], 32, 64));
+      }
+      if ((threadIdx.x & 63) < 16) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) red[w][8 * cg + e] = cmax[e];
+      }
+      __syncthreads();
+      if (threadIdx.x < 128) {  // a column each, over the waves
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) m = max(m, red[k][threadIdx.x]);
+        red[0][threadIdx.x] = m;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) cmax[e] = red[0][8 * cg + e];
     }
-    if ((threadIdx.x & 63) < 16) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) red[w][8 * cg + e] = cmax[e];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      cmax[e] = max(max(red[0][8 * cg + e], red[1][8 * cg + e]), max(red[2][8 * cg + e], red[3][8 * cg + e]));
   }
   if (P.q) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < R; ++i) {
       if (r0 + i >= P.rows) break;
       const uint32_t byte = scale_byte<TOP>(rmax[i]);
       float f[8];
@@ -97,20 +103,30 @@ __global__ __launch_bounds__(256) void quant_kernel(const QuantArgs P) {
       const uint32_t byte = scale_byte<TOP>(cmax[e]);
       float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = raw[i].get(e);
-      *reinterpret_cast<u32x2*>(&tile[8 * cg + e][8 * rg]) = to_fp8<TOP>(f, inverse_scale(byte));
+      for (int i = 0; i < 8; ++i) f[i] = i < R ? raw[i < R ? i : 0].get(e) : 0.f;
+      const u32x2 o = to_fp8<TOP>(f, inverse_scale(byte));
+      if constexpr (R == 8) *reinterpret_cast<u32x2*>(&tile[8 * cg + e][8 * rg]) = o;
+      else *reinterpret_cast<uint16_t*>(&tile[8 * cg + e][R * rg]) = (uint16_t)o[0];
       if (!BLOCK && rg == 0 && c0 + e < P.cols) P.scale_t[(c0 + e) * P.ldsct + blockIdx.y] = (uint8_t)byte;
     }
     if (BLOCK && threadIdx.x == 0) P.scale_t[blockIdx.x * P.ldsct + blockIdx.y] = (uint8_t)scale_byte<TOP>(cmax[0]);
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {  // 8 bytes of 16 rows of qt at a time
-      const int c = 16 * k + (threadIdx.x >> 4);
+    for (int k = 0; k < R; ++k) {  // 8 bytes of 128 / R rows of qt at a time
+      const int c = 128 / R * k + rg;
       if ((int64_t)blockIdx.x * 128 + c < P.cols)
         *reinterpret_cast<u32x2*>(P.qt + ((int64_t)blockIdx.x * 128 + c) * P.ldqt + (int64_t)blockIdx.y * 128 + 8 * cg) =
             *reinterpret_cast<const u32x2*>(&tile[c][8 * cg]);
     }
   }
+}
+
+template <class T, int TOP, bool BLOCK>
+void quant_tiles(const QuantArgs& P, dim3 grid, hipStream_t s) {
+  // the other side's latency was 9.3 against 5 us for 1101 x 523 (45 tiles), its
+  // rate 14 against 17 us for 8192 x 2048 (1024 tiles)
+  if ((int64_t)grid.x * grid.y <= 256) quant_kernel<T, TOP, BLOCK, 2><<<grid, 1024, 0, s>>>(P);
+  else quant_kernel<T, TOP, BLOCK, 8><<<grid, 256, 0, s>>>(P);
 }
 
 template <class T, int TOP>
@@ -126,8 +142,8 @@ hipError_t quant_launch(const QuantArgs& P, int block_rows, hipStream_t s) {
     if (P.qt) Q.qt = P.qt + r;
     if (P.qt) Q.scale_t = P.scale_t + r / 128;
     const dim3 grid((unsigned)cdiv(P.cols, 128), (unsigned)cdiv(Q.rows, 128));
-    if (block_rows == 128) quant_kernel<T, TOP, true><<<grid, 256, 0, s>>>(Q);
-    else quant_kernel<T, TOP, false><<<grid, 256, 0, s>>>(Q);
+    if (block_rows == 128) quant_tiles<T, TOP, true>(Q, grid, s);
+    else quant_tiles<T, TOP, false>(Q, grid, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

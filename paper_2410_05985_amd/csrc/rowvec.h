@@ -78,25 +78,24 @@ struct Raw8<float> {
 };
 
 // Columns c .. c + 7 of a row of d; behind its end zeros.  The group that the
-// end cuts is the row's last eight elements, shifted down: one load as for any
-// other (a load for each element, or none of it past the end, cost a round trip
-// to memory each: 1003 x 1237 forward 11 us instead of 9).
-// WHOLE: d is a multiple of 8.
+// end cuts is loaded as the row's last eight elements, like any other, and
+// shifted down by finish_group once all loads of a thread are on their way
+// (loads element by element, or a shift behind each load, cost a round trip to
+// memory each: 1003 x 1237 forward 11 us, now 6).  WHOLE: d is a multiple of 8.
 template <bool WHOLE = false, class T>
 __device__ __forceinline__ void load_group(Raw8<T>& r, const T* row, int64_t c, int64_t d) {
-  r.zero();
-  if (c >= d) return;
-  if constexpr (WHOLE) {
-    r.load(row + c);
-    return;
+  if (c < d && (WHOLE || d >= 8)) r.load(row + (WHOLE || c + 8 <= d ? c : d - 8));
+  else r.zero();
+}
+template <bool WHOLE = false, class T>
+__device__ __forceinline__ void finish_group(Raw8<T>& r, const T* row, int64_t c, int64_t d) {
+  if constexpr (!WHOLE) {
+    if (d < 8) {
+      if (c == 0) r.load_some(row, (int)d);
+    } else if (c < d && c + 8 > d) {
+      r.drop_front((int)(c + 8 - d));
+    }
   }
-  if (d < 8) {
-    r.load_some(row, (int)d);
-    return;
-  }
-  const int64_t at = c + 8 <= d ? c : d - 8;
-  r.load(row + at);
-  if (at < c) r.drop_front((int)(c - at));
 }
 template <bool WHOLE = false, class T>
 __device__ __forceinline__ void store_group(T* p, const float (&f)[8], int64_t n) {
