@@ -196,9 +196,9 @@ layup_status layup_refresh_shadow(layup_ctx* ctx);
  * and offset = step * (2 n_layer + 1) + site, where step counts the context's
  * completed steps and site is 0 for the embeddings, 1 + 2l and 2 + 2l for
  * block l's attention and MLP: a step repeated from the same state draws the
- * same masks, and the backward draws the forward's.  p = 0 (the initial state)
- * turns dropout off.  0 <= p < 1.  LAYUP_ERR_STATE between a forward and the
- * end of its backward; LAYUP_ERR_DTYPE for the MLP. */
+ * same masks.  A backward draws its forward's masks, whatever was set since.
+ * p = 0 (the initial state) turns dropout off.  0 <= p < 1; LAYUP_ERR_DTYPE for
+ * the MLP. */
 layup_status layup_set_dropout(layup_ctx* ctx, float p, uint64_t seed);
 
 /* Forward pass and loss (Algorithm 1 "Forward pass"), followed by the
@@ -474,8 +474,8 @@ layup_status layup_gemm_f32(const layup_gemm_desc* d, void* stream);
  * on its device, whatever the current device.  Nothing is allocated and no
  * state is kept between calls: calls on different streams are independent as
  * long as their buffers (workspaces included) are, and every call can be
- * captured into a graph.  Results are the same bit for bit in every run.
- * Errors through layup_global_error.  Buffers may overlap only as stated. */
+ * captured into a graph.  A call's results are the same bit for bit in every
+ * run (a row's last bits may depend on how many rows the call has).  Errors through layup_global_error.  Buffers may overlap only as stated. */
 
 typedef enum {
   LAYUP_F32 = 0,
@@ -565,7 +565,8 @@ layup_status layup_layernorm_forward(const layup_layernorm_desc* d, void* stream
  * that reaches s past the LayerNorm.  s, dsum and dres have s_dtype.  dres, dx,
  * dgamma, dbeta are nullable.  dgamma and dbeta (float32 [d]) are overwritten,
  * and zeroed for rows = 0; they need workspace
- * (layup_layernorm_workspace_size bytes, 16-byte aligned).  dres may be dsum's
+ * (layup_layernorm_workspace_size bytes, 16-byte aligned; fewer rows never need
+ * more).  dres may be dsum's
  * own buffer (same ld). */
 typedef struct {
   int64_t rows;
@@ -607,7 +608,7 @@ layup_status layup_layernorm_workspace_size(int64_t rows, int32_t d, size_t* byt
  *      its own (its blocks run along x's rows), laid out the same way; with
  *      block_rows = 128 its values are those of q.
  * ld_scale (bytes) is a multiple of 4 and at least the number of blocks of a
- * row, scale 4-byte aligned.  x is float32 or bfloat16.  rows = 0 or cols = 0
+ * row, scale 4-byte aligned; layup_gemm_fp8 reads a row's bytes four at a time.  x is float32 or bfloat16.  rows = 0 or cols = 0
  * is a no-op. */
 typedef struct {
   int64_t rows, cols;

@@ -181,9 +181,8 @@ struct layup_ctx {
   int next_backward = -1;
   std::vector<char> backward_done;
   int32_t step_index = 0;  // value written to the trace
-  // dropout (layup_set_dropout), and as the forward in flight took it
-  float drop_p = 0.f;
-  uint64_t drop_seed = 0, drop_first = 0;  // drop_first: offset of the step's site 0
+  layup_dropout_mask drop{};  // dropout of the next forward (layup_set_dropout)
+  Mask drop_mask{};           // and of the one in flight: offset is the step's site 0
   bool drop_on = false;
   bool dx_valid = false;   // dx[cur_dx] holds the input gradient of the last backwarded unit
   // workspace
@@ -440,11 +439,9 @@ int64_t attention_site(int l) { return 1 + 2 * l; }
 int64_t mlp_site(int l) { return 2 + 2 * l; }
 
 Mask site_mask(const layup_ctx* c, int64_t site) {
-  layup_dropout_mask m{};
-  m.p = c->drop_p;
-  m.seed = c->drop_seed;
-  m.offset = c->drop_first + (uint64_t)site;
-  return make_mask(m);
+  Mask m = c->drop_mask;
+  m.offset += (uint64_t)site;
+  return m;
 }
 
 // The residual add and dropout in front of a LayerNorm and the LayerNorm, in
@@ -1117,8 +1114,9 @@ layup_status layup_forward(layup_ctx* ctx, const int32_t* tokens, const float* x
   ctx->timeline_valid = false;
   ctx->dx_valid = false;
   ctx->tokens = tokens;
-  ctx->drop_on = site_mask(ctx, 0).thr != 0;
-  ctx->drop_first = (uint64_t)ctx->step_index * (uint64_t)(2 * ctx->cfg.n_layer + 1);
+  ctx->drop_mask = make_mask(ctx->drop);
+  ctx->drop_mask.offset = (uint64_t)ctx->step_index * (uint64_t)(2 * ctx->cfg.n_layer + 1);
+  ctx->drop_on = ctx->drop_mask.thr != 0;
   layup_status st = ctx->cfg.model == LAYUP_MODEL_GPT_BF16 ? gpt_forward(ctx, tokens, loss_out)
                                                             : mlp_forward(ctx, tokens, x, loss_out);
   if (st != LAYUP_OK) return st;
@@ -1132,9 +1130,8 @@ layup_status layup_set_dropout(layup_ctx* ctx, float p, uint64_t seed) {
   if (!ctx) return fail(nullptr, LAYUP_ERR_INVALID_ARG, "null context");
   if (ctx->cfg.model != LAYUP_MODEL_GPT_BF16) return fail(ctx, LAYUP_ERR_DTYPE, "dropout is for the GPT model");
   if (!(p >= 0.f && p < 1.f)) return fail(ctx, LAYUP_ERR_INVALID_ARG, "dropout probability must be at least 0 and below 1");
-  if (ctx->forward_done) return fail(ctx, LAYUP_ERR_STATE, "dropout changed between a forward and its backward");
-  ctx->drop_p = p;
-  ctx->drop_seed = seed;
+  ctx->drop.p = p;
+  ctx->drop.seed = seed;
   return LAYUP_OK;
 }
 

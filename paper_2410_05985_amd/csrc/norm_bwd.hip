@@ -166,18 +166,18 @@ __global__ __launch_bounds__(SUM_COLS * SUM_LANES) void norm_sum_kernel(const fl
   }
 }
 
-// Blocks of the backward (and partial rows).
-static int64_t bwd_blocks(int64_t rows, int d) {
+// Blocks of the backward (and partial rows): two a CU.
+constexpr int64_t MAX_PARTS = 512;
+int64_t norm_partial_rows(int64_t rows, int d) {
   const int tpr = team_of(rows, d), rpb = threads_of(tpr) / tpr;
-  return std::min<int64_t>(cdiv(rows, rpb), 512);
+  return std::min<int64_t>(cdiv(rows, rpb), MAX_PARTS);
 }
-
-int64_t norm_partial_rows(int64_t rows, int d) { return bwd_blocks(rows, d); }
-int64_t norm_partial_floats(int64_t rows, int d) { return bwd_blocks(rows, d) * 2 * (int64_t)d; }
+// Room for them, whatever the team: more rows never need less.
+int64_t norm_partial_floats(int64_t rows, int d) { return std::min(rows, MAX_PARTS) * 2 * (int64_t)d; }
 
 template <class TY, class TS, class TX, int TPR, int NV, bool WHOLE>
 static hipError_t bwd_launch(const BwdArgs& P, hipStream_t s) {
-  norm_bwd_kernel<TY, TS, TX, TPR, NV, WHOLE><<<(unsigned)bwd_blocks(P.rows, P.d), threads_of(TPR), 0, s>>>(P);
+  norm_bwd_kernel<TY, TS, TX, TPR, NV, WHOLE><<<(unsigned)norm_partial_rows(P.rows, P.d), threads_of(TPR), 0, s>>>(P);
   return hipGetLastError();
 }
 template <class TY, class TS, class TX>
@@ -233,7 +233,7 @@ hipError_t launch_norm_bwd(const layup_layernorm_grad_desc& d, const Mask& k, hi
   }
   if (!sums) return hipSuccess;
   norm_sum_kernel<<<(unsigned)cdiv(2 * d.d, SUM_COLS), SUM_COLS * SUM_LANES, 0, s>>>(
-      (const float*)d.workspace, (int)bwd_blocks(d.rows, d.d), d.d, d.dgamma, d.dbeta);
+      (const float*)d.workspace, (int)norm_partial_rows(d.rows, d.d), d.d, d.dgamma, d.dbeta);
   return hipGetLastError();
 }
 

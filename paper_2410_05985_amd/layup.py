@@ -466,6 +466,22 @@ def _same_type(*ts):
     return codes.pop() if codes else None
 
 
+def _keep(d, *tensors):
+    """Keeps the descriptor's tensors, which are on one device; the calls refuse those in host memory."""
+    d.kept = tensors
+    devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
+    if len(devices) > 1:
+        raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
+    d.in_host_memory = any(x.type == "cpu" for x in devices)
+    return d
+
+
+def _call(f, desc, stream):
+    if getattr(desc, "in_host_memory", False):
+        raise ValueError("tensors in host memory")
+    _check(f(C.byref(desc), _stream(stream)))
+
+
 def _mask(p, seed, offset, offset_dev) -> layup_dropout_mask:
     if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
         raise ValueError("seed and offset are unsigned 64-bit numbers")
@@ -479,12 +495,11 @@ def dropout_desc(x, y, p: float, seed: int = 0, offset: int = 0, offset_dev=None
     d.y, d.ldy = _matrix(y, x.shape)
     d.dtype = _same_type(x, y)
     d.drop = _mask(p, seed, offset, offset_dev)
-    d.kept = (x, y, offset_dev)
-    return d
+    return _keep(d, x, y, offset_dev)
 
 
 def layup_dropout(desc: layup_dropout_desc, stream=None):
-    _check(lib().layup_dropout(C.byref(desc), _stream(stream)))
+    _call(lib().layup_dropout, desc, stream)
 
 
 def layernorm_desc(x, y, gamma=None, beta=None, residual=None, sum_out=None, mean=None, rstd=None, eps: float = 1e-5,
@@ -509,12 +524,11 @@ def layernorm_desc(x, y, gamma=None, beta=None, residual=None, sum_out=None, mea
     d.gamma, d.beta = (_vector(v, d.d, "torch.float32") for v in (gamma, beta))
     d.mean, d.rstd = (_vector(v, d.rows, "torch.float32") for v in (mean, rstd))
     d.drop = _mask(p, seed, offset, offset_dev)
-    d.kept = (x, y, gamma, beta, residual, sum_out, mean, rstd, y_scale, offset_dev)
-    return d
+    return _keep(d, x, y, gamma, beta, residual, sum_out, mean, rstd, y_scale, offset_dev)
 
 
 def layup_layernorm_forward(desc: layup_layernorm_desc, stream=None):
-    _check(lib().layup_layernorm_forward(C.byref(desc), _stream(stream)))
+    _call(lib().layup_layernorm_forward, desc, stream)
 
 
 def layup_layernorm_workspace_size(rows: int, d: int) -> int:
@@ -540,12 +554,11 @@ def layernorm_grad_desc(dy, s, mean, rstd, gamma=None, dsum=None, dres=None, dx=
     if workspace is not None:
         d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     d.drop = _mask(p, seed, offset, offset_dev)
-    d.kept = (dy, s, mean, rstd, gamma, dsum, dres, dx, dgamma, dbeta, workspace, offset_dev)
-    return d
+    return _keep(d, dy, s, mean, rstd, gamma, dsum, dres, dx, dgamma, dbeta, workspace, offset_dev)
 
 
 def layup_layernorm_backward(desc: layup_layernorm_grad_desc, stream=None):
-    _check(lib().layup_layernorm_backward(C.byref(desc), _stream(stream)))
+    _call(lib().layup_layernorm_backward, desc, stream)
 
 
 def _eight(q, rows: int, k: int):
@@ -577,12 +590,11 @@ def quant_desc(x, block_rows: int, q=None, scale=None, qt=None, scale_t=None) ->
     if qt is not None:
         d.qt, d.ldqt = _eight(qt, cols, rows)
         d.scale_t, d.ld_scale_t = _scale(scale_t, -(-cols // max(1, block_rows)), rows)
-    d.kept = (x, q, scale, qt, scale_t)
-    return d
+    return _keep(d, x, q, scale, qt, scale_t)
 
 
 def layup_quant_fp8(desc: layup_quant_desc, stream=None):
-    _check(lib().layup_quant_fp8(C.byref(desc), _stream(stream)))
+    _call(lib().layup_quant_fp8, desc, stream)
 
 
 def gemm_fp8_desc(A, a_scale, a_block: int, B, b_scale, b_block: int, C_, K: int, bias=None,
@@ -600,12 +612,11 @@ def gemm_fp8_desc(A, a_scale, a_block: int, B, b_scale, b_block: int, C_, K: int
     d.bias = _vector(bias, d.N, "torch.float32")
     if workspace is not None:
         d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    d.kept = (A, a_scale, B, b_scale, C_, bias, workspace)
-    return d
+    return _keep(d, A, a_scale, B, b_scale, C_, bias, workspace)
 
 
 def layup_gemm_fp8(desc: layup_gemm_fp8_desc, stream=None):
-    _check(lib().layup_gemm_fp8(C.byref(desc), _stream(stream)))
+    _call(lib().layup_gemm_fp8, desc, stream)
 
 
 # ------------------------------------------------------------- harness

@@ -38,9 +38,7 @@ def test_units_teacher_forced(cfg, p):
     torch.cuda.synchronize()
     LU.layup_set_dropout(m.ctx, p, seed)
     LU.layup_forward(m.ctx, td, None, None)
-    with pytest.raises(LU.LayupError) as e:
-        LU.layup_set_dropout(m.ctx, 0.0, seed)  # its backward is still to come
-    assert e.value.status == LU.LAYUP_ERR_STATE
+    LU.layup_set_dropout(m.ctx, 0.7, seed + 1)  # for the next forward: this one's backward keeps its masks
     m.synchronize()
     idx = tokens[:, :cfg.seq].reshape(-1)
     emb = pf["wte"][idx] + pf["wpe"][np.tile(np.arange(cfg.seq), cfg.batch)]
@@ -136,6 +134,34 @@ def test_off_is_the_step_without():
     assert np.array_equal(want, run_steps(S.GPT_TEST, 1e-6, 5))
     assert np.array_equal(want, run_steps(S.GPT_TEST, 0.0, 5, first=(0.5, 7)))
     assert not np.array_equal(want, run_steps(S.GPT_TEST, 0.1, 5))
+
+
+def test_evaluation_between_steps():
+    """Dropout off for a forward that has no backward, and on again: the next step is as if it had not been."""
+    cfg = S.GPT_TEST
+    outs, losses = [], []
+    for evaluate in (False, True):
+        params, tokens, peers, m = gpt_setup(cfg)
+        td = torch.from_numpy(tokens).to(DEV)
+        loss = torch.zeros(1, dtype=torch.float32, device=DEV)
+        for s in range(2):
+            hp, _ = gpt_hp(cfg, s + 1)
+            if evaluate:
+                LU.layup_set_dropout(m.ctx, 0.0, 0)
+                torch.cuda.synchronize()
+                LU.layup_forward(m.ctx, td, None, loss)
+                m.synchronize()
+                losses.append(loss.item())
+            LU.layup_set_dropout(m.ctx, 0.3, 8)
+            torch.cuda.synchronize()
+            LU.layup_step(m.ctx, td, None, hp, cfg.alpha, 0)
+        m.synchronize()
+        outs.append(m.params.cpu().numpy().copy())
+        if evaluate:
+            ref = O.gpt_forward({k: v.astype(np.float64) for k, v in params.items()}, tokens, cfg.n_head)[0]
+            assert abs(losses[0] - ref) <= 2e-3 * abs(ref)
+        m.close()
+    assert np.array_equal(outs[0], outs[1])
 
 
 @pytest.mark.parametrize("cfg", [S.GPT_TEST, S.GPT_TEST4], ids=lambda c: c.name)

@@ -630,3 +630,46 @@ def test_calls_on_two_streams_do_not_meet():
     for _, _, outs in sets:
         for a, b in zip(outs, want):
             assert torch.equal(a, b)
+
+
+# --------------------------------------------------------- beyond 32 bits
+
+
+def test_offsets_beyond_32_bits():
+    """Rows so far apart, or so many, that element and byte offsets pass 2^32: the last rows come out as they do alone."""
+    rows, d, far = 70_001, 200, 1 << 16
+    x = torch.empty(rows, far, dtype=BF16, device=DEV)[:, :d]  # 9.2 GB, 4.6e9 elements
+    x.normal_()
+    y = torch.empty(rows, d, dtype=BF16, device=DEV)
+    LU.layup_dropout(LU.dropout_desc(x, y, p=0.3, seed=2, offset=5))
+    tail = slice(rows - 3, rows)
+    keep = torch.from_numpy(R.keep_mask(3, d, 0.3, 2, 5, row0=rows - 3)).to(DEV)
+    ref = torch.where(keep, x[tail].float() * np.float32(R.drop_scale(0.3)), torch.zeros((), device=DEV)).to(BF16)
+    assert torch.equal(y[tail], ref)
+    # LayerNorm, and its backward with the weight's gradient over all rows
+    g = torch.ones(d, device=DEV)
+    far_y = torch.empty(rows, far, dtype=BF16, device=DEV)[:, :d]
+    mean, rstd = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    LU.layup_layernorm_forward(LU.layernorm_desc(x, far_y, g, g, mean=mean, rstd=rstd))
+    ref, _, _ = R.norm_fwd(f64(x[tail]), 1.0, 1.0, 1e-5)
+    near(f64(far_y[tail]), ref, 1e-5 * (1 + np.abs(ref)) + 2.0 ** -8 * np.abs(ref), "y")
+    ws = torch.empty(LU.layup_layernorm_workspace_size(rows, d), dtype=torch.uint8, device=DEV)
+    db = torch.empty(d, device=DEV)
+    LU.layup_layernorm_backward(LU.layernorm_grad_desc(far_y, x, mean, rstd, g, dx=y, dbeta=db, workspace=ws))
+    total = far_y.double()
+    near(f64(db), total.sum(0).cpu().numpy(), 300 * U * total.abs().sum(0).cpu().numpy(), "dbeta")
+    del far_y, total
+    # 8-bit rows 65536 bytes apart; the product's last rows of A and of B
+    q = torch.zeros(rows, far, dtype=torch.uint8, device=DEV).view(FP8["e4m3"])
+    e = torch.zeros(rows, 4, dtype=torch.uint8, device=DEV)
+    LU.layup_quant_fp8(LU.quant_desc(x, 1, q=q, scale=e))
+    vq, ve = R.quantise(f64(x[tail]), "e4m3", 1)
+    assert np.array_equal(q[tail].view(torch.uint8)[:, :d].contiguous().view(FP8["e4m3"]).double().cpu().numpy(), vq)
+    assert np.array_equal(e[tail, :2].cpu().numpy(), ve)
+    few_q, few_e = q[tail].contiguous(), e[tail].contiguous()
+    v = R.value(vq, ve, 1)
+    for a, ea, b, eb in ((q, e, few_q, few_e), (few_q, few_e, q, e)):
+        c = torch.empty(a.shape[0], b.shape[0], device=DEV)
+        LU.layup_gemm_fp8(LU.gemm_fp8_desc(a, ea, 1, b, eb, 1, c, d))
+        got = c[tail] if a is q else c[:, tail]
+        near(f64(got), v @ v.T, product_bound(v, v, F32), "product")

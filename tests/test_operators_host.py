@@ -123,6 +123,9 @@ def test_layernorm_workspace():
             LU.layup_layernorm_workspace_size(rows, d)
         assert e.value.status == SHAPE
     assert LU.layup_layernorm_workspace_size(0, 8) == 0
+    for d in (8, 300, 768, 1000, 2048, 5000, 16384):  # sized for the largest batch, it serves the smaller ones
+        sizes = [LU.layup_layernorm_workspace_size(r, d) for r in (1, 7, 96, 128, 129, 511, 513, 768, 769, 4000, 8192)]
+        assert sizes == sorted(sizes)
     assert LU.layup_layernorm_workspace_size(8192, 768) >= 2 * 768 * 4
 
 
@@ -163,3 +166,7 @@ def test_descriptors_from_tensors():
     with pytest.raises(ValueError):
         LU.gemm_fp8_desc(q, e, 1, q, e, 1, torch.zeros(5, 6), 12)  # B has five rows, C six columns
     assert LU.gemm_fp8_desc(q, e, 1, q, e, 1, torch.zeros(5, 5), 12).c_f32 == 1
+    with pytest.raises(ValueError):
+        LU.dropout_desc(x, x.to("meta"), p=0.5)  # two devices
+    with pytest.raises(ValueError):
+        LU.layup_dropout(LU.dropout_desc(x, x, p=0.5))  # host memory
