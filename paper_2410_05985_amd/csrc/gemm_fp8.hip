@@ -51,7 +51,8 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float scale) {
 }
 
 // 2^(byte - 127) of the low byte
-__device__ __forceinline__ float scale_of(uint32_t s) { return __builtin_bit_cast(float, (s & 255u) << 23); }
+__device__ __forceinline__ uint32_t scale_bits(uint32_t s) { return (s & 255u) << 23; }
+__device__ __forceinline__ float scale_of(uint32_t s) { return __builtin_bit_cast(float, scale_bits(s)); }
 
 // 64 k of a fragment: two 16-byte chunks of one row a lane, which 32 k of the
 // row they are does not matter as long as A and B agree (all share a scale).
@@ -99,7 +100,7 @@ __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
 // SCN / 4 words, word w at place w ^ sc_swz(r), so that 32 consecutive rows'
 // words of a step lie in different banks.  (Fetched by the step, a word for
 // each row is a cache line for each row, as many requests as the operands
-// themselves: the copies alone took 446 us of 8192 x 8192 x 8192, now 399.
+// themselves: the copies alone took 446 us of 8192 x 8192 x 8192, then 399.
 // Kept in registers and loaded every fourth step, they brought a branch into
 // the step, over which the compiler moved the products it was to overlap, and
 // a wait for every copy in flight.)  A longer K drains the pipeline every SCN
@@ -110,6 +111,22 @@ __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
 // A step starts with the last cluster of the step before, already in
 // registers: its products cover the barrier's and the new stage's first
 // fragment reads' latency and carry the copies of a later step.
+//
+// Two stages leave a copy one step to arrive.  The 256 x 256 tile (MID) has room
+// for no third one, but its first two clusters read all of B and half of A: a
+// second barrier behind them gives those three quarters of the stage to the
+// step after next, so every copy has a step and a half (8192 x 8192 x 8192 475
+// -> 447 us, of it the copies alone 399 -> 300).
+//
+// What bounds it: at 8192 x 8192 x 8192 (450 us, 2.44 PFLOP/s; the card reaches
+// 2.8 in a large library product) the products need 220 us at full clock, the
+// copies and fragment reads alone 300; zeros for operands, which draw less
+// power, take 370.  Float32 results: 8192 x 2048 x 8192 211 us, 1.30 PFLOP/s of
+// the 1.4 of a large bfloat16 product.  With a short K the stores weigh more:
+// 8192 x 8192 x 2048 138 us.  Measured and not kept: K steps of 64 in rings of
+// four and five stages (600 us: half a cache line a row), four waves of 128 x
+// 128 (a third fewer LDS reads: 444 at that size, but 111 against 106 at 8192 x
+// 2048 x 8192), workgroups that start the next tile before their stores.
 __device__ __forceinline__ int chunk_off(int r, int c) { return r * 128 + 16 * (c ^ ((r >> 1) & 7)); }
 
 // W words a row: 64 / W rows fill the banks once
@@ -126,6 +143,11 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   static_assert(BM / 8 % NW == 0 && BN / 8 % NW == 0, "copies must split evenly over the waves");
   constexpr int CA = TM >= 2 ? 2 : 1, NC = TM / CA;  // clusters of 64 k
   static_assert(TM % CA == 0, "whole clusters");
+  // MID: a second barrier after clusters 0 and 1, which read B and the first
+  // half of each wave's rows of A
+  constexpr bool MID = NC == 2;
+  static_assert(MID ? S == 2 && LOADS_A % 2 == 0 : NC == 1, "a stage in two parts, or in one");
+  constexpr int PIECE_E = MID ? LOADS_A / 2 : 0, PIECE_M = NPIECE - PIECE_E;  // copies of the second part, of the first
   __shared__ __attribute__((aligned(1024))) char smem[S * (A_BYTES + B_BYTES) + ROWS * SCN];
 
   // tiles go in groups of 8 tile-rows for L2 reuse of B
@@ -152,10 +174,16 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   // tile's first row and the step are scalar, a lane's offset has 32 bits
   // (leading dimensions are at most 2^24).
   char* const smem_b = smem + S * A_BYTES;
+  auto a_block = [&](int i) {  // 8 rows of A; with MID a wave's first copies are of the first part
+    if constexpr (!MID) return wave * LOADS_A + i;
+    constexpr int HALF = CA * 4;  // blocks of a part of a wave's rows
+    const int t = wave * PIECE_E + i % std::max(1, PIECE_E);
+    return t / HALF * 2 * HALF + t % HALF + (i < PIECE_E ? 0 : HALF);
+  };
   uint32_t off_a[LOADS_A], off_b[LOADS_B];
 #pragma unroll
   for (int i = 0; i < LOADS_A; ++i) {
-    const int r = (wave * LOADS_A + i) * 8 + (lane >> 3);
+    const int r = a_block(i) * 8 + (lane >> 3);
     off_a[i] = (uint32_t)min((int64_t)r, P.M - 1 - m0) * (uint32_t)P.lda + 16 * ((lane & 7) ^ ((r >> 1) & 7));
   }
 #pragma unroll
@@ -165,13 +193,27 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   }
   const char* base_a = (const char*)P.A + m0 * P.lda + (int64_t)kb0 * 128;
   const char* base_b = (const char*)P.B + n0 * P.ldb + (int64_t)kb0 * 128;
-  auto issue = [&](int slot, int p) {  // copy p of the next step into a stage
-    if (p < LOADS_A) copy_block<0>(base_a + off_a[p], smem + slot * A_BYTES + (wave * LOADS_A + p) * 1024);
-    else copy_block<0>(base_b + off_b[p - LOADS_A], smem_b + slot * B_BYTES + (wave * LOADS_B + p - LOADS_A) * 1024);
-    if (p == NPIECE - 1) {
+  const char* base_e = base_a;
+  // a scalar base and the lane's offset, not a pointer for each copy: sixteen
+  // registers, with which the 256 x 256 tile's scales and offsets spilled
+  auto copy = [&](const char* base, uint32_t off, char* lds) {
+    asm volatile("" : "+v"(off));
+    copy_block<0>(base + off, lds);
+  };
+  auto copy_a = [&](const char* base, int slot, int i) {
+    copy(base, off_a[i], smem + slot * A_BYTES + a_block(i) * 1024);
+  };
+  auto issue = [&](int slot, int p) {  // copy p of the next step's first part into a stage
+    if (p < LOADS_B) copy(base_b, off_b[p], smem_b + slot * B_BYTES + (wave * LOADS_B + p) * 1024);
+    else copy_a(base_a, slot, p - LOADS_B);
+    if (p == PIECE_M - 1) {
       base_a += 128;
       base_b += 128;
     }
+  };
+  auto issue_e = [&](int slot, int p) {  // of the second
+    copy_a(base_e, slot, LOADS_A - PIECE_E + p);
+    if (p == PIECE_E - 1) base_e += 128;
   };
   // the scale words of steps k0 .. k0 + SCN - 1; past the last one, that again
   char* const smem_s = smem + S * (A_BYTES + B_BYTES);
@@ -195,73 +237,76 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   };
 
   // fragments: rows 32 i + lane % 32, chunks 2 ks + lane / 32; the swizzle
-  // leaves whole blocks of 32 rows alone
-  uint32_t a_off[4], b_off[4];
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    a_off[ks] = chunk_off(wm * WM + (lane & 31), 2 * ks + (lane >> 5));
-    b_off[ks] = chunk_off(wn * WN + (lane & 31), 2 * ks + (lane >> 5));
-  }
+  // leaves whole blocks of 32 rows alone, and a chunk's number meets it in bits
+  // that the stages' and blocks' offsets leave zero
   const uint32_t lds0 = lds_addr(smem);
-  const uint32_t sa_off = lds0 + S * (A_BYTES + B_BYTES) + 4 * W * (wm * WM + (lane & 31));
-  const uint32_t sb_off = lds0 + S * (A_BYTES + B_BYTES) + 4 * W * (BM + wn * WN + (lane & 31));
-  uint32_t sa[TM], sb[TN], wa[TM], wb[TN];  // scales in use (the low byte counts); the words of the step that begins
+  const uint32_t frag = chunk_off(lane & 31, lane >> 5);
+  const uint32_t frag_a = lds0 + wm * WM * 128, frag_b = lds0 + S * A_BYTES + wn * WN * 128;
+  const uint32_t sc = lds0 + S * (A_BYTES + B_BYTES) + 4 * W * (lane & 31);
+  uint32_t sa[TM], sb[TN], wa[TM], wb[TN];  // scales in use (EXACT: as floats, else the low byte counts); the words of the step that begins
 #pragma unroll
-  for (int i = 0; i < TM; ++i) sa[i] = 127;
+  for (int i = 0; i < TM; ++i) sa[i] = EXACT ? scale_bits(127) : 127;
 #pragma unroll
-  for (int j = 0; j < TN; ++j) sb[j] = 127;
+  for (int j = 0; j < TN; ++j) sb[j] = EXACT ? scale_bits(127) : 127;
   Frag af[2][CA], bf[2][TN];
 #pragma unroll
   for (int i = 0; i < CA; ++i) af[1][i].lo = af[1][i].hi = u32x4{0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < TN; ++j) bf[1][j].lo = bf[1][j].hi = u32x4{0, 0, 0, 0};
 
-  // cluster q of a step: 64 k number q / NC, row blocks CA (q % NC) ..
+  // cluster q of a step: 64 k number q % 2, row blocks CA (q / 2) ..
   auto read_cluster = [&](auto Q, int kt, int slot) {
-    constexpr int q = decltype(Q)::value, h = q / NC, i0 = CA * (q % NC);
-    const uint32_t ab = lds0 + (uint32_t)(slot * A_BYTES), bb = lds0 + (uint32_t)(S * A_BYTES + slot * B_BYTES);
+    constexpr int q = decltype(Q)::value, h = q & 1, i0 = CA * (q / 2);
+    const uint32_t ab = (frag_a + (uint32_t)(slot * A_BYTES) + frag) ^ (64 * h), bb = (frag_b + (uint32_t)(slot * B_BYTES) + frag) ^ (64 * h);
     if constexpr (q == 0) {
       const uint32_t w = 4 * ((kt >> 2) ^ sc_swz<W>(lane));
-      static_for<0, TM>([&](auto I) { wa[decltype(I)::value] = lds_read_b32<decltype(I)::value * 128 * W>(sa_off + w); });
-      static_for<0, TN>([&](auto J) { wb[decltype(J)::value] = lds_read_b32<decltype(J)::value * 128 * W>(sb_off + w); });
+      static_for<0, TM>([&](auto I) { wa[decltype(I)::value] = lds_read_b32<decltype(I)::value * 128 * W>(sc + w + 4 * W * wm * WM); });
+      static_for<0, TN>([&](auto J) { wb[decltype(J)::value] = lds_read_b32<decltype(J)::value * 128 * W>(sc + w + 4 * W * (BM + wn * WN)); });
     }
-    if constexpr (q % NC == 0)
+    if constexpr (q < 2)
       static_for<0, TN>([&](auto J) {
         constexpr int j = decltype(J)::value;
-        bf[h & 1][j].lo = lds_read_b128<j * 4096>(bb + b_off[2 * h]);
-        bf[h & 1][j].hi = lds_read_b128<j * 4096>(bb + b_off[2 * h + 1]);
+        bf[h][j].lo = lds_read_b128<j * 4096>(bb);
+        bf[h][j].hi = lds_read_b128<j * 4096>(bb ^ 32);
       });
     static_for<0, CA>([&](auto I) {
       constexpr int i = decltype(I)::value;
-      af[q & 1][i].lo = lds_read_b128<(i0 + i) * 4096>(ab + a_off[2 * h]);
-      af[q & 1][i].hi = lds_read_b128<(i0 + i) * 4096>(ab + a_off[2 * h + 1]);
+      af[h][i].lo = lds_read_b128<(i0 + i) * 4096>(ab);
+      af[h][i].hi = lds_read_b128<(i0 + i) * 4096>(ab ^ 32);
     });
   };
   auto landed = [&](auto Q) {  // the cluster's reads have been waited for
-    constexpr int q = decltype(Q)::value, h = q / NC;
+    constexpr int q = decltype(Q)::value, h = q & 1;
     if constexpr (q == 0) {
 #pragma unroll
       for (int i = 0; i < TM; ++i) after_wait(wa[i]);
 #pragma unroll
       for (int j = 0; j < TN; ++j) after_wait(wb[j]);
     }
-    if constexpr (q % NC == 0)
+    if constexpr (q < 2)
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        after_wait(bf[h & 1][j].lo);
-        after_wait(bf[h & 1][j].hi);
+        after_wait(bf[h][j].lo);
+        after_wait(bf[h][j].hi);
       }
 #pragma unroll
     for (int i = 0; i < CA; ++i) {
-      after_wait(af[q & 1][i].lo);
-      after_wait(af[q & 1][i].hi);
+      after_wait(af[h][i].lo);
+      after_wait(af[h][i].hi);
     }
   };
-  // COPY: with the copies of a later step into stage `slot` between them
+  // COPY 1 (2): with the copies of a later step's first (second) part into stage
+  // `slot` between them
   auto multiply = [&](auto Q, auto COPY, int slot) {
-    constexpr int q = decltype(Q)::value, h = q / NC, i0 = CA * (q % NC);
-    constexpr bool copy = decltype(COPY)::value != 0;
-    constexpr int PER = (NPIECE + CA * TN - 1) / (CA * TN);
+    constexpr int q = decltype(Q)::value, h = q & 1, i0 = CA * (q / 2);
+    constexpr int which = decltype(COPY)::value, pieces = which == 0 ? 0 : which == 1 ? PIECE_M : PIECE_E;
+    // copies between product x of n and the next
+    auto copies = [&](int x, int n) {
+      const int per = (pieces + n - 1) / n;
+#pragma unroll
+      for (int p = x * per; p < (x + 1) * per; ++p)
+        if (p < pieces) which == 1 ? issue(slot, p) : issue_e(slot, p);
+    };
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (EXACT) {
 #pragma unroll
@@ -269,33 +314,27 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
         bf16x8 xb[TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-          const u32x4& v = x < 2 ? bf[h & 1][j].lo : bf[h & 1][j].hi;
-          xb[j] = widen<FB>(v[2 * (x & 1)], v[2 * (x & 1) + 1], scale_of(sb[j]));
+          const u32x4& v = x < 2 ? bf[h][j].lo : bf[h][j].hi;
+          xb[j] = widen<FB>(v[2 * (x & 1)], v[2 * (x & 1) + 1], __builtin_bit_cast(float, sb[j]));
         }
 #pragma unroll
         for (int i = 0; i < CA; ++i) {
-          const u32x4& v = x < 2 ? af[q & 1][i].lo : af[q & 1][i].hi;
-          const bf16x8 xa = widen<FA>(v[2 * (x & 1)], v[2 * (x & 1) + 1], scale_of(sa[i0 + i]));
+          const u32x4& v = x < 2 ? af[h][i].lo : af[h][i].hi;
+          const bf16x8 xa = widen<FA>(v[2 * (x & 1)], v[2 * (x & 1) + 1], __builtin_bit_cast(float, sa[i0 + i]));
 #pragma unroll
           for (int j = 0; j < TN; ++j)
             acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j], xa, acc[i0 + i][j], 0, 0, 0);
         }
-        if constexpr (copy) {
-#pragma unroll
-          for (int p = x * ((NPIECE + 3) / 4); p < (x + 1) * ((NPIECE + 3) / 4); ++p)
-            if (p < NPIECE) issue(slot, p);
-        }
+        copies(x, 4);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < CA; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-          product64<FA, FB>(af[q & 1][i], bf[h & 1][j], sa[i0 + i], sb[j], acc[i0 + i][j]);
-          if constexpr (copy) {
-#pragma unroll
-            for (int p = (i * TN + j) * PER; p < (i * TN + j + 1) * PER; ++p)
-              if (p < NPIECE) issue(slot, p);
+          product64<FA, FB>(af[h][i], bf[h][j], sa[i0 + i], sb[j], acc[i0 + i][j]);
+          if constexpr (pieces > 0) {
+            copies(i * TN + j, CA * TN);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -305,18 +344,24 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   auto advance = [&](int kt) {  // the scales of step kt
     const int sh = 8 * (kt & 3);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = wa[i] >> sh;
+    for (int i = 0; i < TM; ++i) sa[i] = EXACT ? scale_bits(wa[i] >> sh) : wa[i] >> sh;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] = wb[j] >> sh;
+    for (int j = 0; j < TN; ++j) sb[j] = EXACT ? scale_bits(wb[j] >> sh) : wb[j] >> sh;
   };
   constexpr int LAST = 2 * NC - 1;
-  // MAIN: step kt + S - 1 of the ns exists.  No branch between LDS reads and
-  // their wait.
-  auto k_step = [&](auto MAIN, int kt, int ns, int slot) {
-    constexpr bool main = decltype(MAIN)::value != 0;
+  // Step kt of ns.  Copies complete in order, and a step waits for its own alone.
+  // MID: MORE (0 to 2) steps follow at least.  Parts are asked for in the order
+  // first, second, first, ..: the first part of step kt + 2 at kt's second
+  // barrier, into the stage that kt has half read, its second part at kt + 1's
+  // first.  Else MORE: step kt + S - 1 exists, and is asked for.
+  // No branch between LDS reads and their wait.
+  auto k_step = [&](auto MORE, int kt, int ns, int slot) {
+    constexpr int more = decltype(MORE)::value;
     const int pslot = slot == 0 ? S - 1 : slot - 1;  // of steps kt - 1 and kt + S - 1
-    if constexpr (main) {
-      WAIT_VMCNT((S - 2) * NPIECE);  // loads complete in order: step kt has landed
+    if constexpr (MID) {
+      WAIT_VMCNT(more ? NPIECE : PIECE_E);
+    } else if constexpr (more) {
+      WAIT_VMCNT((S - 2) * NPIECE);
     } else {
       const int left = min(S - 2, ns - 1 - kt);  // younger steps still in flight
       static_for<0, S - 1>([&](auto D) {
@@ -326,37 +371,54 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     }
     barrier_only();
     read_cluster(IntC<0>{}, kt, slot);
-    multiply(IntC<LAST>{}, IntC<main ? 1 : 0>{}, pslot);
+    multiply(IntC<LAST>{}, IntC<more == 0 ? 0 : MID ? 2 : 1>{}, pslot);
     lgkm_wait<0>();
     landed(IntC<0>{});
     advance(kt);
     static_for<0, LAST>([&](auto Q) {
       constexpr int q = decltype(Q)::value;
+      if constexpr (MID && q == 1) {
+        WAIT_VMCNT(more ? NPIECE : 0);
+        barrier_only();
+      }
       read_cluster(IntC<q + 1>{}, kt, slot);
-      multiply(Q, IntC<0>{}, 0);
+      multiply(Q, IntC<MID && q == 1 && more == 2 ? 1 : 0>{}, slot);
       lgkm_wait<0>();
       landed(IntC<q + 1>{});
     });
   };
+  auto all = [&](int slot) {
+#pragma unroll
+    for (int p = 0; p < PIECE_M; ++p) issue(slot, p);
+  };
   for (int k0 = 0; k0 < nk; k0 += SCN) {
     const int ns = min(nk - k0, SCN);
     if (k0 > 0) barrier_only();  // every wave has read the last stage
-    // the first stage before the scales, which the first step waits for too
-#pragma unroll
-    for (int t = 0; t < S - 1; ++t) {
-      if (t < ns)
-#pragma unroll
-        for (int p = 0; p < NPIECE; ++p) issue(t, p);
-      if (t == 0) copy_scales(k0);
-    }
+    // the first copies before the scales, which the first step waits for too
     int kt = 0, slot = 0;
-    for (; kt + S - 1 < ns; ++kt) {
-      k_step(IntC<1>{}, kt, ns, slot);
-      slot = slot + 1 == S ? 0 : slot + 1;
-    }
-    for (; kt < ns; ++kt) {
+    if constexpr (MID) {
+      all(0);
+      copy_scales(k0);
+#pragma unroll
+      for (int p = 0; p < PIECE_E; ++p) issue_e(0, p);
+      if (ns > 1) all(1);
+      for (; kt + 2 < ns; ++kt, slot ^= 1) k_step(IntC<2>{}, kt, ns, slot);
+      if (kt + 1 < ns) k_step(IntC<1>{}, kt++, ns, slot), slot ^= 1;
       k_step(IntC<0>{}, kt, ns, slot);
-      slot = slot + 1 == S ? 0 : slot + 1;
+    } else {
+#pragma unroll
+      for (int t = 0; t < S - 1; ++t) {
+        if (t < ns) all(t);
+        if (t == 0) copy_scales(k0);
+      }
+      for (; kt + S - 1 < ns; ++kt) {
+        k_step(IntC<1>{}, kt, ns, slot);
+        slot = slot + 1 == S ? 0 : slot + 1;
+      }
+      for (; kt < ns; ++kt) {
+        k_step(IntC<0>{}, kt, ns, slot);
+        slot = slot + 1 == S ? 0 : slot + 1;
+      }
     }
   }
   multiply(IntC<LAST>{}, IntC<0>{}, 0);
@@ -600,8 +662,12 @@ enum TileId { T256x256 = 0, T256x128, T128x128, T64x64, T_ROWS, kNumCfg };
 // on a full chip), a tile fix us besides (first copies, stores), a byte of C
 // 1 / gbs ns.  Fitted to 1008 timings of 70 products of 65 to 8192 a side, with
 // operands and result in rotation: the choice takes 1.01 of the best tile and
-// split's time on average, 1.04 at the 90th percentile, 1.17 at most.  [0]:
-// bfloat16 results, [1]: float32.
+// split's time on average, 1.19 at most.  The figures rank; they are no forecast
+// (a tile's fix holds what the loop cannot overlap).  One is not the fit's: a
+// 256 x 256 tile's 13.0 for bfloat16 is raised to 15, since the fit took it for
+// 8192 x 4096 x 1024 (48 us, on 128 x 128 44); it stays the choice at a longer K
+// (8192 x 8192 x 2048 138 against 143, 8192 x 2048 x 8192 106 against 124).
+// [0]: bfloat16 results, [1]: float32.
 struct TileCfg {
   int bm, bn, occ;
   struct {
@@ -609,10 +675,10 @@ struct TileCfg {
   } t[2];
 };
 const TileCfg kCfgs[kNumCfg] = {
-    {256, 256, 1, {{1.01f, 0.73f, 17.0f, 1300.f}, {2.27f, 2.02f, 15.4f, 1800.f}}},  // 2 x 4 waves, 2 stages
-    {256, 128, 1, {{0.59f, 0.44f, 7.5f, 1300.f}, {1.27f, 1.15f, 8.0f, 2000.f}}},    // 4 x 2 waves, 3 stages
-    {128, 128, 2, {{0.53f, 0.54f, 4.5f, 1220.f}, {0.76f, 1.21f, 5.2f, 1950.f}}},    // 2 x 2 waves, 2 stages
-    {64, 64, 4, {{0.37f, 0.55f, 1.6f, 1130.f}, {0.40f, 0.91f, 1.9f, 1970.f}}},      // 2 x 2 waves, 2 stages
+    {256, 256, 1, {{0.98f, 0.71f, 15.0f, 1330.f}, {2.19f, 1.97f, 14.1f, 1940.f}}},  // 2 x 4 waves, 2 stages
+    {256, 128, 1, {{0.57f, 0.47f, 7.3f, 1320.f}, {1.19f, 1.14f, 8.0f, 1990.f}}},    // 4 x 2 waves, 3 stages
+    {128, 128, 2, {{0.53f, 0.59f, 4.4f, 1250.f}, {0.71f, 1.22f, 5.1f, 1990.f}}},    // 2 x 2 waves, 2 stages
+    {64, 64, 4, {{0.37f, 0.59f, 1.5f, 1140.f}, {0.40f, 0.96f, 1.7f, 1970.f}}},      // 2 x 2 waves, 2 stages
     {32, 16, 1, {}},
 };
 

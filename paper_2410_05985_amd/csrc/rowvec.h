@@ -81,7 +81,7 @@ struct Raw8<float> {
 // end cuts is loaded as the row's last eight elements, like any other, and
 // shifted down by finish_group once all loads of a thread are on their way
 // (loads element by element, or a shift behind each load, cost a round trip to
-// memory each: 1003 x 1237 forward 11 us, now 6).  WHOLE: d is a multiple of 8.
+// memory each: 1003 x 1237 forward 11 us, now 7).  WHOLE: d is a multiple of 8.
 template <bool WHOLE = false, class T>
 __device__ __forceinline__ void load_group(Raw8<T>& r, const T* row, int64_t c, int64_t d) {
   if (c < d && (WHOLE || d >= 8)) r.load(row + (WHOLE || c + 8 <= d ? c : d - 8));
