@@ -116,7 +116,14 @@ __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
 // for no third one, but its first two clusters read all of B and half of A: a
 // second barrier behind them gives those three quarters of the stage to the
 // step after next, so every copy has a step and a half (8192 x 8192 x 8192 475
-// -> 447 us, of it the copies alone 399 -> 300).
+// -> 447 us, of it the copies alone 399 -> 300).  Where a wave's rows are
+// one cluster (EARLY), it reads both halves of k before it multiplies the first,
+// and the barrier behind them gives the whole stage away: two steps for a copy,
+// at the price of a wait for a cluster's reads (700 x 1000 x 4300 on 64 x 64 19.6 ->
+// 14.0 us; where the chip is full 8192 x 8192 x 2048 on 128 x 128 150 -> 148).
+// Widening makes the products so long that copies arrive anyway: 128 x 128 with
+// float32 results lost (4096 x 1024 x 8192 62.5 -> 68.5 us) and keeps one
+// barrier, 64 x 64 gained (700 x 1000 x 4300 20.3 -> 17.5).
 //
 // What bounds it: at 8192 x 8192 x 8192 (450 us, 2.44 PFLOP/s; the card reaches
 // 2.8 in a large library product) the products need 220 us at full clock, the
@@ -143,9 +150,8 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   static_assert(BM / 8 % NW == 0 && BN / 8 % NW == 0, "copies must split evenly over the waves");
   constexpr int CA = TM >= 2 ? 2 : 1, NC = TM / CA;  // clusters of 64 k
   static_assert(TM % CA == 0, "whole clusters");
-  // MID: a second barrier after clusters 0 and 1, which read B and the first
-  // half of each wave's rows of A
-  constexpr bool MID = NC == 2;
+  // MID, EARLY: a second barrier in a step
+  constexpr bool MID = NC == 2, EARLY = NC == 1 && S == 2 && (!EXACT || TM * TN == 1), TWO = MID || EARLY;
   static_assert(MID ? S == 2 && LOADS_A % 2 == 0 : NC == 1, "a stage in two parts, or in one");
   constexpr int PIECE_E = MID ? LOADS_A / 2 : 0, PIECE_M = NPIECE - PIECE_E;  // copies of the second part, of the first
   __shared__ __attribute__((aligned(1024))) char smem[S * (A_BYTES + B_BYTES) + ROWS * SCN];
@@ -350,15 +356,15 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   };
   constexpr int LAST = 2 * NC - 1;
   // Step kt of ns.  Copies complete in order, and a step waits for its own alone.
-  // MID: MORE (0 to 2) steps follow at least.  Parts are asked for in the order
+  // TWO: MORE (0 to 2) steps follow at least.  Parts are asked for in the order
   // first, second, first, ..: the first part of step kt + 2 at kt's second
-  // barrier, into the stage that kt has half read, its second part at kt + 1's
-  // first.  Else MORE: step kt + S - 1 exists, and is asked for.
+  // barrier, into the stage that kt has read (MID: half read), its second part
+  // at kt + 1's first.  Else MORE: step kt + S - 1 exists, and is asked for.
   // No branch between LDS reads and their wait.
   auto k_step = [&](auto MORE, int kt, int ns, int slot) {
     constexpr int more = decltype(MORE)::value;
     const int pslot = slot == 0 ? S - 1 : slot - 1;  // of steps kt - 1 and kt + S - 1
-    if constexpr (MID) {
+    if constexpr (TWO) {
       WAIT_VMCNT(more ? NPIECE : PIECE_E);
     } else if constexpr (more) {
       WAIT_VMCNT((S - 2) * NPIECE);
@@ -371,7 +377,7 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     }
     barrier_only();
     read_cluster(IntC<0>{}, kt, slot);
-    multiply(IntC<LAST>{}, IntC<more == 0 ? 0 : MID ? 2 : 1>{}, pslot);
+    multiply(IntC<LAST>{}, IntC<more == 0 ? 0 : TWO ? 2 : 1>{}, pslot);
     lgkm_wait<0>();
     landed(IntC<0>{});
     advance(kt);
@@ -382,9 +388,16 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
         barrier_only();
       }
       read_cluster(IntC<q + 1>{}, kt, slot);
-      multiply(Q, IntC<MID && q == 1 && more == 2 ? 1 : 0>{}, slot);
-      lgkm_wait<0>();
-      landed(IntC<q + 1>{});
+      if constexpr (EARLY) {
+        lgkm_wait<0>();
+        landed(IntC<q + 1>{});
+        barrier_only();
+        multiply(Q, IntC<more == 2 ? 1 : 0>{}, slot);
+      } else {
+        multiply(Q, IntC<MID && q == 1 && more == 2 ? 1 : 0>{}, slot);
+        lgkm_wait<0>();
+        landed(IntC<q + 1>{});
+      }
     });
   };
   auto all = [&](int slot) {
@@ -396,7 +409,7 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     if (k0 > 0) barrier_only();  // every wave has read the last stage
     // the first copies before the scales, which the first step waits for too
     int kt = 0, slot = 0;
-    if constexpr (MID) {
+    if constexpr (TWO) {
       all(0);
       copy_scales(k0);
 #pragma unroll
@@ -662,11 +675,11 @@ enum TileId { T256x256 = 0, T256x128, T128x128, T64x64, T_ROWS, kNumCfg };
 // on a full chip), a tile fix us besides (first copies, stores), a byte of C
 // 1 / gbs ns.  Fitted to 1008 timings of 70 products of 65 to 8192 a side, with
 // operands and result in rotation: the choice takes 1.01 of the best tile and
-// split's time on average, 1.19 at most.  The figures rank; they are no forecast
+// split's time on average, 1.25 at most.  The figures rank; they are no forecast
 // (a tile's fix holds what the loop cannot overlap).  One is not the fit's: a
 // 256 x 256 tile's 13.0 for bfloat16 is raised to 15, since the fit took it for
-// 8192 x 4096 x 1024 (48 us, on 128 x 128 44); it stays the choice at a longer K
-// (8192 x 8192 x 2048 138 against 143, 8192 x 2048 x 8192 106 against 124).
+// 8192 x 4096 x 1024 (47 us, on 128 x 128 42); it stays the choice at a longer K
+// (8192 x 2048 x 8192 104 us against 124).
 // [0]: bfloat16 results, [1]: float32.
 struct TileCfg {
   int bm, bn, occ;
@@ -675,10 +688,10 @@ struct TileCfg {
   } t[2];
 };
 const TileCfg kCfgs[kNumCfg] = {
-    {256, 256, 1, {{0.98f, 0.71f, 15.0f, 1330.f}, {2.19f, 1.97f, 14.1f, 1940.f}}},  // 2 x 4 waves, 2 stages
-    {256, 128, 1, {{0.57f, 0.47f, 7.3f, 1320.f}, {1.19f, 1.14f, 8.0f, 1990.f}}},    // 4 x 2 waves, 3 stages
-    {128, 128, 2, {{0.53f, 0.59f, 4.4f, 1250.f}, {0.71f, 1.22f, 5.1f, 1990.f}}},    // 2 x 2 waves, 2 stages
-    {64, 64, 4, {{0.37f, 0.59f, 1.5f, 1140.f}, {0.40f, 0.96f, 1.7f, 1970.f}}},      // 2 x 2 waves, 2 stages
+    {256, 256, 1, {{0.98f, 0.69f, 15.0f, 1340.f}, {2.19f, 1.92f, 14.1f, 1920.f}}},  // 2 x 4 waves, 2 stages
+    {256, 128, 1, {{0.57f, 0.45f, 7.3f, 1320.f}, {1.19f, 1.11f, 8.0f, 1990.f}}},    // 4 x 2 waves, 3 stages
+    {128, 128, 2, {{0.42f, 0.57f, 5.0f, 1360.f}, {0.70f, 1.17f, 5.1f, 1980.f}}},    // 2 x 2 waves, 2 stages
+    {64, 64, 4, {{0.25f, 0.53f, 1.8f, 1200.f}, {0.35f, 0.92f, 2.0f, 2000.f}}},      // 2 x 2 waves, 2 stages
     {32, 16, 1, {}},
 };
 
