@@ -475,7 +475,8 @@ layup_status layup_gemm_f32(const layup_gemm_desc* d, void* stream);
  * state is kept between calls: calls on different streams are independent as
  * long as their buffers (workspaces included) are, and every call can be
  * captured into a graph.  A call's results are the same bit for bit in every
- * run (a row's last bits may depend on how many rows the call has).  Errors through layup_global_error.  Buffers may overlap only as stated. */
+ * run (a row's last bits may depend on how many rows the call has).  Errors
+ * through layup_global_error.  Buffers may overlap only as stated. */
 
 typedef enum {
   LAYUP_F32 = 0,
@@ -566,8 +567,7 @@ layup_status layup_layernorm_forward(const layup_layernorm_desc* d, void* stream
  * dgamma, dbeta are nullable.  dgamma and dbeta (float32 [d]) are overwritten,
  * and zeroed for rows = 0; they need workspace
  * (layup_layernorm_workspace_size bytes, 16-byte aligned; fewer rows never need
- * more).  dres may be dsum's
- * own buffer (same ld). */
+ * more).  dres may be dsum's own buffer (same ld). */
 typedef struct {
   int64_t rows;
   int32_t d;
@@ -608,8 +608,8 @@ layup_status layup_layernorm_workspace_size(int64_t rows, int32_t d, size_t* byt
  *      its own (its blocks run along x's rows), laid out the same way; with
  *      block_rows = 128 its values are those of q.
  * ld_scale (bytes) is a multiple of 4 and at least the number of blocks of a
- * row, scale 4-byte aligned; layup_gemm_fp8 reads a row's bytes four at a time.  x is float32 or bfloat16.  rows = 0 or cols = 0
- * is a no-op. */
+ * row, scale 4-byte aligned; layup_gemm_fp8 reads a row's bytes four at a
+ * time.  x is float32 or bfloat16.  rows = 0 or cols = 0 is a no-op. */
 typedef struct {
   int64_t rows, cols;
   const void* x;
@@ -641,8 +641,8 @@ layup_status layup_quant_fp8(const layup_quant_desc* d, void* stream);
  * W [out, in]: the forward is A = x, B = W; dX is A = dY, B = W^T (quantised
  * over out); dW is A = dY^T, B = x^T (both quantised over the tokens).  Each
  * operand is E4M3 or E5M2.  lda, ldb: at least K rounded up to 128, multiples
- * of 16, at most 2^24 (as the scales' rows); A and B 16-byte aligned; scales as layup_quant_fp8 states (bytes 1 to
- * 254).
+ * of 16, at most 2^24 (as the scales' rows); A and B 16-byte aligned; scales as
+ * layup_quant_fp8 states (bytes 1 to 254).
  * workspace (device, optional, 16-byte aligned): float32 split-K partials; K is
  * split only when they fit, and the summation order, and so the rounding, then
  * differ.  M = 0 or N = 0 is a no-op; K = 0 writes C = bias (or 0). */

@@ -473,6 +473,28 @@ def test_product_tiles(tile, M, N, K, splits, out):
             cfg=TILES[tile], splits=splits)
 
 
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("K", [4096, 4100, 4300, 4500, 8300])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_product_tiles_start_anew_after_32_steps(tile, K, out):
+    """The scales of 32 steps of 128 k are staged at a time: a last round of 32, 1, 2, 4 and 1 steps."""
+    product(130, 270, K, "e5m2", "e4m3", 1, 128 if out == BF16 else 1, out=out, cfg=TILES[tile], spread=0.5)
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_product_tiles_agree_bit_for_bit(out):
+    """Every tile adds k in the same order, on a full chip too: the same bits each time."""
+    M, N, K = 2300, 2100, 1500
+    first, desc = product(M, N, K, out=out, cfg=0)
+    first = first.clone()
+    for tile in TILES.values():
+        for _ in range(3):
+            desc.kept[4].zero_()
+            tile_call(desc, tile, 1)
+            torch.cuda.synchronize()
+            assert torch.equal(desc.kept[4], first), tile
+
+
 @pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 31, 32])
 @pytest.mark.parametrize("N,K", [(1, 1), (33, 128), (100, 500), (64, 640), (257, 2048), (96, 9000)])
 @pytest.mark.parametrize("out", [BF16, F32])
