@@ -22,7 +22,9 @@ struct BwdArgs {
 // of partial sums a block goes to memory, which norm_sum_kernel adds (atomics
 // would add them in another order each time).  Bound by HBM: 8192 x 8192, five
 // bfloat16 streams, 132 us (5.1 TB/s) and the sums 8; 8192 x 768 with a float32
-// residual stream 22 us (4.6 TB/s) and the sums 4.
+// residual stream 22 us (4.6 TB/s) and the sums 4.  The next row's loads before
+// this row's sums were measured: 1237 columns 41.3 -> 37.7 us, 8192 columns 141
+// -> 140, a float32 stream of 2048 columns 55 -> 56, 768 columns 22 -> 24; not kept.
 // WHOLE: d is a multiple of 8.
 template <class TY, class TS, class TX, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(const BwdArgs P) {

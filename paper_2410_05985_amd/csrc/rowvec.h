@@ -97,6 +97,10 @@ __device__ __forceinline__ void finish_group(Raw8<T>& r, const T* row, int64_t c
     }
   }
 }
+// Stores around the caches are not used: alone they gain (8192 x 768 forward and
+// backward 45 -> 43 us, an 8192 x 2048 quantiser 14.9 -> 12.9), but whoever reads
+// the result next pays for it (a linear layer's operands and products, 8192 x
+// 4096 x 1024: 192 -> 216).
 template <bool WHOLE = false, class T>
 __device__ __forceinline__ void store_group(T* p, const float (&f)[8], int64_t n) {
   if (WHOLE || n >= 8) Raw8<T>::store(p, f);
