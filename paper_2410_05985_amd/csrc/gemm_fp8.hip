@@ -440,13 +440,14 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   // ---- epilogue, from the registers.  A lane has columns 8 q + 4 (l/32) ..+3
   // of row l%32 for q = 0..3; exchanges between lane groups gather 16 bytes of
   // a row in a lane and 64 bytes of it in four lanes, so a store covers sixteen
-  // rows' 64-byte pieces.
+  // rows' 64-byte pieces.  The pieces carry the alignment of one element (element
+  // by element 8192 x 2303 x 768 took 66 us, now 39; 2304 columns 24); what the
+  // last column cuts goes by the element.
   const bool part = P.splits > 1;
   const bool wide = part || EXACT;  // float32 stores
   float* const cf = part ? P.partial + (int64_t)split * P.M * P.N : (float*)P.C;
   const int64_t ldc = part ? P.N : P.ldc;
   const float* const bias = part ? nullptr : P.bias;
-  const bool vec = ((uintptr_t)(part ? (void*)P.partial : P.C) & 15) == 0 && (ldc & 7) == 0 && (P.N & 7) == 0;
   const int hf = lane >> 5, l16 = (lane >> 4) & 1, l4 = lane & 15;
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
@@ -469,17 +470,7 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int64_t nb = n0 + wn * WN + j * 32;
-      if (!vec) {
-        const int64_t m = mb + (lane & 31);
-        if (m < P.M)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int64_t n = nb + 8 * (r >> 2) + 4 * hf + (r & 3);
-            if (n >= P.N) continue;
-            if (wide) cf[m * ldc + n] = acc[i][j][r];
-            else ((bf16_t*)P.C)[m * ldc + n] = f2bf(acc[i][j][r]);
-          }
-      } else if (wide) {
+      if (wide) {
         // q pairs: columns 16 p .. + 15
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
@@ -492,9 +483,18 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
             swap16(x[t], y[t]);  // x: rows 0..15, y: rows 16..31; odd lane groups: columns 8 ..
           }
           const int64_t n = nb + 16 * p + 8 * l16 + 4 * hf;
-          if (n < P.N) {
-            if (mb + l4 < P.M) *reinterpret_cast<u32x4*>(cf + (mb + l4) * ldc + n) = u32x4{x[0], x[1], x[2], x[3]};
-            if (mb + 16 + l4 < P.M) *reinterpret_cast<u32x4*>(cf + (mb + 16 + l4) * ldc + n) = u32x4{y[0], y[1], y[2], y[3]};
+          typedef u32x4 V __attribute__((aligned(4)));
+          uint32_t* const to = reinterpret_cast<uint32_t*>(cf + (mb + l4) * ldc + n);
+          uint32_t* const to2 = to + 16 * ldc;
+          if (n + 4 <= P.N) {
+            if (mb + l4 < P.M) *reinterpret_cast<V*>(to) = u32x4{x[0], x[1], x[2], x[3]};
+            if (mb + 16 + l4 < P.M) *reinterpret_cast<V*>(to2) = u32x4{y[0], y[1], y[2], y[3]};
+          } else if (n < P.N) {
+#pragma unroll
+            for (int t = 0; t < 3; ++t) {
+              if (n + t < P.N && mb + l4 < P.M) to[t] = x[t];
+              if (n + t < P.N && mb + 16 + l4 < P.M) to2[t] = y[t];
+            }
           }
         }
       } else {
@@ -512,21 +512,29 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) swap16(w[0][t], w[1][t]);  // w[y]: row 16 y + l%16, columns 16 (l/16 odd) + 8 (l/32)
         const int64_t n = nb + 16 * l16 + 8 * hf;
-        if (n < P.N)
+        typedef u32x4 V __attribute__((aligned(2)));
+        bf16_t* const to[2] = {(bf16_t*)P.C + (mb + l4) * ldc + n, (bf16_t*)P.C + (mb + 16 + l4) * ldc + n};
+        if (n + 8 <= P.N) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const int64_t m = mb + 16 * y + l4;
-            if (m >= P.M) continue;
-            const u32x4 v{w[y][0], w[y][1], w[y][2], w[y][3]};
-            u32x4* const to = reinterpret_cast<u32x4*>((bf16_t*)P.C + m * ldc + n);
+            if (mb + 16 * y + l4 >= P.M) continue;
+            const V v = u32x4{w[y][0], w[y][1], w[y][2], w[y][3]};
             if (P.past) {
               asm volatile("");  // or the two stores become one, without the hint
-              __builtin_nontemporal_store(v, to);
+              __builtin_nontemporal_store(v, reinterpret_cast<V*>(to[y]));
               asm volatile("");
             } else {
-              *to = v;
+              *reinterpret_cast<V*>(to[y]) = v;
             }
           }
+        } else if (n < P.N) {
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            if (mb + 16 * y + l4 < P.M)
+#pragma unroll
+              for (int t = 0; t < 7; ++t)
+                if (n + t < P.N) to[y][t] = (bf16_t)(w[y][t >> 1] >> (16 * (t & 1)));
+        }
       }
     }
   }
@@ -769,7 +777,9 @@ hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits
   // behind its LayerNorm 43.7 us, else 49.1; 8192 x 4096 x 1024 with a reader of
   // the result 68, else 74).  From 96 MB on the product gains nothing and its
   // reader loses (8192 x 8192 x 2048, 134 MB, with a reader 212 us, else 186).
-  P.past = P.M * P.N <= (48ll << 20);
+  // Rows that do not start on 16 bytes share lines with their neighbours, whose
+  // parts the caches join (8192 x 2303 x 768 39 us, past them 47).
+  P.past = P.M * P.N <= (48ll << 20) && P.ldc % 8 == 0 && ((uintptr_t)P.C & 15) == 0;
   if (P.kb == 0) {
     if (P.M * P.N >= (1ll << 31) * 256ll) return hipErrorInvalidValue;
     fp8_bias_kernel<<<(unsigned)cdiv(P.M * P.N, 256), 256, 0, s>>>(P);
