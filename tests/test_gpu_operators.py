@@ -481,6 +481,19 @@ def test_product_tiles_start_anew_after_32_steps(tile, K, out):
     product(130, 270, K, "e5m2", "e4m3", 1, 128 if out == BF16 else 1, out=out, cfg=TILES[tile], spread=0.5)
 
 
+@pytest.mark.parametrize("M,N", [(70, 64), (133, 201), (9, 40)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_product_into_memory_aligned_to_its_elements(M, N, out):
+    """The same bits one element off a 16-byte boundary as on it, and nothing around the result is written."""
+    c, desc = product(M, N, 640, out=out)
+    a, ea, b, eb, _, bias, _ = desc.kept
+    room = torch.full((M * N + 2,), 7.0, dtype=out, device=DEV)
+    off = room[1:-1].view(M, N)
+    LU.layup_gemm_fp8(LU.gemm_fp8_desc(a, ea, 1, b, eb, 128, off, 640, bias=bias), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert torch.equal(off, c) and room[0] == 7.0 and room[-1] == 7.0
+
+
 @pytest.mark.parametrize("out", [BF16, F32])
 def test_product_tiles_agree_bit_for_bit(out):
     """Every tile adds k in the same order, on a full chip too: the same bits each time."""
