@@ -11,7 +11,12 @@
 // rounding of a bfloat16 result (1.7e-3), but fifty times a float32 sum's
 // error.  So a float32 result (EXACT) is computed from the operands widened in
 // registers to bfloat16, which holds them exactly, scale included, at the
-// bfloat16 instructions' half rate.
+// bfloat16 instructions' half rate.  Its range ends before the least values
+// times the least scales and the largest times the largest: a wave that meets
+// such a scale byte computes its results again from the values alone
+// (plain_sum; 4096 x 1024 x 8192 with one in every row 6.7 ms, else 66 us.
+// Watching for them costs up to 4 %: 1 x 2048 x 8192 7.4 -> 7.7 us, 2048 x 2048 x
+// 2048 21.7 -> 22.5, 4000 x 4000 x 16384 398 -> 402).
 #include "lds_pipe.h"
 
 namespace layup {
@@ -54,6 +59,44 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float scale) {
 // 2^(byte - 127) of the low byte
 __device__ __forceinline__ uint32_t scale_bits(uint32_t s) { return (s & 255u) << 23; }
 __device__ __forceinline__ float scale_of(uint32_t s) { return __builtin_bit_cast(float, scale_bits(s)); }
+
+// bfloat16 holds every value of either format (E4M3 2^-9 to 1.75 2^8, E5M2
+// 2^-16 to 1.75 2^15) times the scales of bytes 10 to 239: from 2^-133, its
+// least subnormal, which conversion and matrix instructions keep, to 1.75 2^127.
+constexpr uint32_t WIDEN_LO = 10, WIDEN_HI = 239;
+__device__ __forceinline__ bool too_wide(uint32_t s) { return (s & 255u) - WIDEN_LO > WIDEN_HI - WIDEN_LO; }
+
+// Two values of the format in float32; H: the upper half of the word.
+template <int F, bool H>
+__device__ __forceinline__ auto values2(uint32_t w) {
+  if constexpr (F == 0) return __builtin_amdgcn_cvt_pk_f32_fp8((int)w, H);
+  else return __builtin_amdgcn_cvt_pk_f32_bf8((int)w, H);
+}
+
+// Blocks k0 .. k0 + nk - 1 of an element of C, for scales that bfloat16 cannot
+// carry: a block's sum without its scales, then times both at once.
+template <int FA, int FB>
+__device__ float plain_sum(const Fp8Args& P, int64_t m, int64_t n, int k0, int nk) {
+  const uint8_t *a = P.A + m * P.lda + (int64_t)k0 * 128, *b = P.B + n * P.ldb + (int64_t)k0 * 128;
+  const uint8_t *sa = P.sa + (m >> P.fa) * P.ldsa + k0, *sb = P.sb + (n >> P.fb) * P.ldsb + k0;
+  float sum = 0.f;
+#pragma unroll 1
+  for (int k = 0; k < nk; ++k, a += 128, b += 128) {
+    float s = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 16) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(a + c), y = *reinterpret_cast<const u32x4*>(b + c);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const auto x0 = values2<FA, false>(x[w]), x1 = values2<FA, true>(x[w]);
+        const auto y0 = values2<FB, false>(y[w]), y1 = values2<FB, true>(y[w]);
+        s = fmaf(x1[1], y1[1], fmaf(x1[0], y1[0], fmaf(x0[1], y0[1], fmaf(x0[0], y0[0], s))));
+      }
+    }
+    sum += ldexpf(s, (int)sa[k] + (int)sb[k] - 254);
+  }
+  return sum;
+}
 
 // 64 k of a fragment: two 16-byte chunks of one row a lane, which 32 k of the
 // row they are does not matter as long as A and B agree (all share a scale).
@@ -141,6 +184,44 @@ __device__ __forceinline__ int chunk_off(int r, int c) { return r * 128 + 16 * (
 template <int W>
 __device__ __forceinline__ int sc_swz(int r) { return (r & 31) / (64 / W); }
 
+// What a workgroup computes.  Tiles go in groups of 8 tile-rows for L2 reuse of B.
+struct Place {
+  int64_t m0, n0;
+  int split, kb0, nk;
+};
+template <int BM, int BN>
+__device__ __forceinline__ Place place(const Fp8Args& P, int lid) {
+  const int n_tiles = P.tiles_m * P.tiles_n;
+  const int split = lid / n_tiles, id = lid % n_tiles;
+  constexpr int GROUP = 8;
+  const int width = GROUP * P.tiles_n;
+  const int first_m = id / width * GROUP, gsz = min(P.tiles_m - first_m, GROUP);
+  const int tm = first_m + (id % width) % gsz, tn = (id % width) / gsz;
+  const int kb0 = split * P.kb_split;
+  return {(int64_t)tm * BM, (int64_t)tn * BN, split, kb0, min(P.kb, kb0 + P.kb_split) - kb0};
+}
+
+// A wave's part of a tile by plain_sum.
+template <int BM, int BN, int WGM, int WGN, int FA, int FB>
+__device__ __forceinline__ void plain_tile() {
+  // the arguments and the place anew, so that the main loop keeps nothing for this
+  const Fp8Args* args = (const Fp8Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  int block = blockIdx.x, thread = threadIdx.x;
+  asm volatile("" : "+s"(args), "+s"(block), "+v"(thread));
+  const Fp8Args& P = *args;
+  const Place at = place<BM, BN>(P, work_item(P.tiles_m * P.tiles_n * P.splits, block));
+  constexpr int WM = BM / WGM, WN = BN / WGN;
+  const int wave = thread >> 6;
+#pragma unroll 1
+  for (int t = thread & 63; t < WM * WN; t += 64) {
+    const int64_t m = at.m0 + wave / WGN * WM + t / WN, n = at.n0 + wave % WGN * WN + t % WN;
+    if (m >= P.M || n >= P.N) continue;
+    const float v = plain_sum<FA, FB>(P, m, n, at.kb0, at.nk);
+    if (P.splits > 1) P.partial[((int64_t)at.split * P.M + m) * P.N + n] = v;
+    else ((float*)P.C)[m * P.ldc + n] = v + (P.bias ? P.bias[n] : 0.f);
+  }
+}
+
 template <int BM, int BN, int WGM, int WGN, int S, int FA, int FB, bool EXACT>
 __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
@@ -157,15 +238,9 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   constexpr int PIECE_E = MID ? LOADS_A / 2 : 0, PIECE_M = NPIECE - PIECE_E;  // copies of the second part, of the first
   __shared__ __attribute__((aligned(1024))) char smem[S * (A_BYTES + B_BYTES) + ROWS * SCN];
 
-  // tiles go in groups of 8 tile-rows for L2 reuse of B
-  const int n_tiles = P.tiles_m * P.tiles_n;
-  const int split = lid / n_tiles, id = lid % n_tiles;
-  constexpr int GROUP = 8;
-  const int width = GROUP * P.tiles_n;
-  const int first_m = id / width * GROUP, gsz = min(P.tiles_m - first_m, GROUP);
-  const int tm = first_m + (id % width) % gsz, tn = (id % width) / gsz;
-  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  const int kb0 = split * P.kb_split, nk = min(P.kb, kb0 + P.kb_split) - kb0;
+  const Place at = place<BM, BN>(P, lid);
+  const int64_t m0 = at.m0, n0 = at.n0;
+  const int split = at.split, kb0 = at.kb0, nk = at.nk;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WGN, wn = wave % WGN;
 
@@ -348,8 +423,15 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     }
     __builtin_amdgcn_sched_barrier(0);
   };
+  uint64_t wide_at = 0;  // lanes with a scale that bfloat16 cannot carry
   auto advance = [&](int kt) {  // the scales of step kt
     const int sh = 8 * (kt & 3);
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) wide_at |= __ballot(too_wide(wa[i] >> sh));
+#pragma unroll
+      for (int j = 0; j < TN; ++j) wide_at |= __ballot(too_wide(wb[j] >> sh));
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = EXACT ? scale_bits(wa[i] >> sh) : wa[i] >> sh;
 #pragma unroll
@@ -436,6 +518,12 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
     }
   }
   multiply(IntC<LAST>{}, IntC<0>{}, 0);
+  if constexpr (EXACT) {
+    if (wide_at) {
+      plain_tile<BM, BN, WGM, WGN, FA, FB>();
+      return;
+    }
+  }
 
   // ---- epilogue, from the registers.  A lane has columns 8 q + 4 (l/32) ..+3
   // of row l%32 for q = 0..3; exchanges between lane groups gather 16 bytes of
@@ -594,11 +682,21 @@ __global__ __launch_bounds__(1024) void gemm_fp8_rows_kernel(const Fp8Args P) {
       c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(words(x), words(y), c, FA, FB, 0, (int)ea, 0, (int)eb);
     }
   };
+  bool wide = false;
   for (int g = wave; 4 * g < P.kb; g += nw) {
     uint32_t wa[TM];
     const uint32_t wb = sb[g];
 #pragma unroll
     for (int i = 0; i < TM; ++i) wa[i] = sa[i][g];
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (4 * g + k >= P.kb) break;
+        wide |= too_wide(wb >> (8 * k));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) wide |= too_wide(wa[i] >> (8 * k));
+      }
+    }
     if (4 * g + 4 <= P.kb) {
       Frag y[4], x[TM][4];
 #pragma unroll
@@ -617,6 +715,20 @@ __global__ __launch_bounds__(1024) void gemm_fp8_rows_kernel(const Fp8Args P) {
 #pragma unroll
         for (int i = 0; i < TM; ++i) block(load(a[i], 4 * g + k), y, wa[i] >> (8 * k), wb >> (8 * k), acc[i]);
       }
+    }
+  }
+  if constexpr (EXACT) {
+    if (__any(wide)) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t m = min((int64_t)16 * i + 4 * (lane >> 4) + r, P.M - 1);
+          float v = 0.f;
+#pragma unroll 1
+          for (int g = wave; 4 * g < P.kb; g += nw) v += plain_sum<FA, FB>(P, m, rb, 4 * g, min(4, P.kb - 4 * g));
+          acc[i][r] = v;
+        }
     }
   }
 #pragma unroll
