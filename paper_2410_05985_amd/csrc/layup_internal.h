@@ -277,6 +277,8 @@ struct Mask {
   const uint64_t* offset_dev;
 };
 Mask make_mask(const layup_dropout_mask& d);
+// Threads that a launch may have along a grid dimension.
+constexpr int64_t MAX_LAUNCH_THREADS = (1ll << 32) - 1;
 hipError_t launch_dropout(const layup_dropout_desc& d, const Mask& k, hipStream_t s);
 constexpr int NORM_MAX_D = 16384;
 hipError_t launch_norm_fwd(const layup_layernorm_desc& d, const Mask& k, hipStream_t s);

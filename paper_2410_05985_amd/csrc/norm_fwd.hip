@@ -67,7 +67,7 @@ struct FwdArgs {
   const float *gamma, *beta;
   float *mean, *rstd;
   uint8_t* yscale;
-  int64_t ldx, ldr, lds, ldy, ldsc, rows;
+  int64_t ldx, ldr, lds, ldy, ldsc, rows, row0;  // row0: the launch's first row
   int32_t d;
   float eps;
   Mask K;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(const FwdArgs
   constexpr bool EARLY = TPR <= 64;
   __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
   const int t = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  const int64_t row = P.row0 + (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
   if (row >= P.rows) return;  // whole teams; a team of several waves is the whole block
   const int d = P.d;
   const TX* x = (const TX*)P.x + row * P.ldx;
@@ -195,9 +195,15 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(const FwdArgs
 }
 
 template <class TX, class TS, int YD, int TPR, int NV, bool WHOLE>
-static hipError_t fwd_launch(const FwdArgs& P, hipStream_t s) {
-  norm_fwd_kernel<TX, TS, YD, TPR, NV, WHOLE><<<(unsigned)cdiv(P.rows, threads_of(TPR) / TPR), threads_of(TPR), 0, s>>>(P);
-  return hipGetLastError();
+static hipError_t fwd_launch(FwdArgs P, hipStream_t s) {
+  constexpr int NT = threads_of(TPR), RPB = NT / TPR;
+  constexpr int64_t most = MAX_LAUNCH_THREADS / NT * RPB;
+  for (; P.row0 < P.rows; P.row0 += most) {
+    norm_fwd_kernel<TX, TS, YD, TPR, NV, WHOLE><<<(unsigned)cdiv(std::min(most, P.rows - P.row0), RPB), NT, 0, s>>>(P);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <class TX, class TS, int YD>
 static hipError_t fwd_width(const FwdArgs& P, hipStream_t s) {
@@ -243,7 +249,7 @@ static hipError_t fwd_type(const FwdArgs& P, int yd, hipStream_t s) {
 
 hipError_t launch_norm_fwd(const layup_layernorm_desc& d, const Mask& k, hipStream_t s) {
   const FwdArgs P{d.x,   d.residual, d.sum, d.y,   d.gamma,    d.beta, d.mean, d.rstd, d.y_scale,
-                  d.ldx, d.ldr,      d.lds, d.ldy, d.ld_scale, d.rows, d.d,    d.eps,  k};
+                  d.ldx, d.ldr,      d.lds, d.ldy, d.ld_scale, d.rows, 0,      d.d,    d.eps, k};
   const bool xf = d.x_dtype == LAYUP_F32, sf = d.s_dtype == LAYUP_F32;
   if (xf) return sf ? fwd_type<float, float>(P, d.y_dtype, s) : fwd_type<float, bf16_t>(P, d.y_dtype, s);
   return sf ? fwd_type<bf16_t, float>(P, d.y_dtype, s) : fwd_type<bf16_t, bf16_t>(P, d.y_dtype, s);

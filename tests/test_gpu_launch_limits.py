@@ -1,0 +1,34 @@
+"""Calls of the documented sizes that need more threads than one launch may have (2^32 along a dimension)."""
+import numpy as np
+import pytest
+
+from oracle import operators_ref as R
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+from paper_2410_05985_amd import layup as LU  # noqa: E402
+from tests.test_gpu_operators import BF16, DEV, U, f64, near  # noqa: E402
+
+
+def test_norm_forward_of_more_rows_than_a_launch_takes():
+    """32 threads a row: 2^27 rows are 2^32 threads.  The rows on both sides of that and the last ones."""
+    rows, d, seed = (1 << 27) + 11, 2, 9
+    x = torch.zeros(rows + 1, d, dtype=BF16, device=DEV)
+    x[-1] = 7.0
+    x[:rows].normal_()
+    y, mean, rstd = (torch.full(s, float("nan"), dtype=t, device=DEV) for s, t in (((rows + 1, d), BF16), ((rows,), torch.float32), ((rows,), torch.float32)))
+    LU.layup_layernorm_forward(LU.layernorm_desc(x[:rows], y[:rows], mean=mean, rstd=rstd, p=0.5, seed=seed), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(y[rows]).all()) and not bool(torch.isnan(mean).any()) and not bool(torch.isnan(y[:rows]).any())
+    for at in (0, (1 << 27) - 16, rows - 16):
+        sl = slice(at, at + 16)
+        s = f64(x[sl]) * R.keep_mask(16, d, 0.5, seed, 0, row0=at) * R.drop_scale(0.5)
+        ref, m, q = R.norm_fwd(s, 1.0, 0.0, 1e-5)
+        # the mean of two terms and a deviation from it are off by at most 2.5 U of the terms' magnitudes, which the
+        # variance takes once more: 5 U times rstd, and a few roundings of y itself
+        total = np.abs(s).sum(1)
+        near(f64(mean[sl]), m, 2 * U * total, "mean")
+        tol = (6 * U * total * q)[:, None] + 8 * U * np.abs(ref)
+        near(f64(y[sl]), ref, tol + 2.0 ** -8 * (np.abs(ref) + tol), f"y at row {at}")
+    del x, y, mean, rstd
+    torch.cuda.empty_cache()
