@@ -131,22 +131,25 @@ void quant_tiles(const QuantArgs& P, dim3 grid, hipStream_t s) {
 
 template <class T, int TOP>
 hipError_t quant_launch(const QuantArgs& P, int block_rows, hipStream_t s) {
-  // at most 65535 tile rows a launch: more go in slices of whole tiles
-  const int64_t most = 65535ll * 128;
-  for (int64_t r = 0; r < P.rows; r += most) {
-    QuantArgs Q = P;
-    Q.rows = std::min(most, P.rows - r);
-    Q.x = (const T*)P.x + r * P.ldx;
-    if (P.q) Q.q = P.q + r * P.ldq;
-    if (P.q) Q.scale = P.scale + r / block_rows * P.ldsc;
-    if (P.qt) Q.qt = P.qt + r;
-    if (P.qt) Q.scale_t = P.scale_t + r / 128;
-    const dim3 grid((unsigned)cdiv(P.cols, 128), (unsigned)cdiv(Q.rows, 128));
-    if (block_rows == 128) quant_tiles<T, TOP, true>(Q, grid, s);
-    else quant_tiles<T, TOP, false>(Q, grid, s);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+  // at most 65535 tile rows a launch, and columns for which its threads (256 a
+  // tile) suffice: more go in slices of whole tiles
+  constexpr int64_t most_r = 65535ll * 128, most_c = MAX_LAUNCH_THREADS / 256 * 128;
+  for (int64_t r = 0; r < P.rows; r += most_r)
+    for (int64_t c = 0; c < P.cols; c += most_c) {
+      QuantArgs Q = P;
+      Q.rows = std::min(most_r, P.rows - r);
+      Q.cols = std::min(most_c, P.cols - c);
+      Q.x = (const T*)P.x + r * P.ldx + c;
+      if (P.q) Q.q = P.q + r * P.ldq + c;
+      if (P.q) Q.scale = P.scale + r / block_rows * P.ldsc + c / 128;
+      if (P.qt) Q.qt = P.qt + c * P.ldqt + r;
+      if (P.qt) Q.scale_t = P.scale_t + c / block_rows * P.ldsct + r / 128;
+      const dim3 grid((unsigned)cdiv(Q.cols, 128), (unsigned)cdiv(Q.rows, 128));
+      if (block_rows == 128) quant_tiles<T, TOP, true>(Q, grid, s);
+      else quant_tiles<T, TOP, false>(Q, grid, s);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   return hipSuccess;
 }
 

@@ -32,3 +32,23 @@ def test_norm_forward_of_more_rows_than_a_launch_takes():
         near(f64(y[sl]), ref, tol + 2.0 ** -8 * (np.abs(ref) + tol), f"y at row {at}")
     del x, y, mean, rstd
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantiser_of_more_columns_than_a_launch_takes(block_rows):
+    """256 threads for 128 columns: 2^31 - 128 columns are as many as a launch takes.  One row of 100 more, its last
+    blocks and some of the first."""
+    cols = (1 << 31) - 28
+    x = torch.empty(1, cols, dtype=BF16, device=DEV).normal_()
+    q = torch.full((1, 1 << 31), 0x55, dtype=torch.uint8, device=DEV)
+    e = torch.full((1, 1 << 24), 0x55, dtype=torch.uint8, device=DEV)
+    LU.layup_quant_fp8(LU.quant_desc(x, block_rows, q=q.view(torch.float8_e4m3fn), scale=e), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for at in (0, (1 << 31) - 512):
+        n = min(512, cols - at)
+        ref, eref = R.quantise(f64(x[:, at:at + n]), "e4m3", block_rows)
+        assert np.array_equal(q[:, at:at + n].contiguous().view(torch.float8_e4m3fn).double().cpu().numpy(), ref), at
+        assert np.array_equal(e[:, at // 128:at // 128 + 4].cpu().numpy(), eref), at
+    assert not bool(q[:, cols:].any())
+    del x, q, e
+    torch.cuda.empty_cache()
