@@ -757,45 +757,46 @@ hipError_t launch_rows(const Fp8Args& P, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Blocks of 256 threads that go through n items at the grid's distance.
+unsigned element_blocks(int64_t n) { return (unsigned)std::min(cdiv(n, 256), MAX_LAUNCH_THREADS / 256); }
+
 // Sum of the split-K partials in split order, bias, rounding: four columns of
 // a row a thread.
 __global__ __launch_bounds__(256) void fp8_reduce_kernel(const Fp8Args P) {
-  const int64_t nq = (P.N + 3) / 4, idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (idx >= P.M * nq) return;
-  const int64_t m = idx / nq, n = (idx - m * nq) * 4, total = P.M * P.N;
-  const float* src = P.partial + m * P.N + n;
-  const int ne = (int)min(P.N - n, (int64_t)4);
-  f32x4 v{0.f, 0.f, 0.f, 0.f};
-  if ((P.N & 3) == 0) {
-    for (int s = 0; s < P.splits; ++s) v += *reinterpret_cast<const f32x4*>(src + s * total);
-  } else {
-    for (int s = 0; s < P.splits; ++s)
+  const int64_t nq = (P.N + 3) / 4, total = P.M * P.N;
+  for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < P.M * nq; idx += (int64_t)gridDim.x * 256) {
+    const int64_t m = idx / nq, n = (idx - m * nq) * 4;
+    const float* src = P.partial + m * P.N + n;
+    const int ne = (int)min(P.N - n, (int64_t)4);
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    if ((P.N & 3) == 0) {
+      for (int s = 0; s < P.splits; ++s) v += *reinterpret_cast<const f32x4*>(src + s * total);
+    } else {
+      for (int s = 0; s < P.splits; ++s)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < ne) v[e] += src[s * total + e];
-  }
+        for (int e = 0; e < 4; ++e)
+          if (e < ne) v[e] += src[s * total + e];
+    }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (e >= ne) break;
-    const float x = v[e] + (P.bias ? P.bias[n + e] : 0.f);
-    if (P.c_f32) ((float*)P.C)[m * P.ldc + n + e] = x;
-    else ((bf16_t*)P.C)[m * P.ldc + n + e] = f2bf(x);
+    for (int e = 0; e < 4; ++e) {
+      if (e >= ne) break;
+      const float x = v[e] + (P.bias ? P.bias[n + e] : 0.f);
+      if (P.c_f32) ((float*)P.C)[m * P.ldc + n + e] = x;
+      else ((bf16_t*)P.C)[m * P.ldc + n + e] = f2bf(x);
+    }
   }
 }
 
 template <int BM, int BN, int WGM, int WGN, int S, int OCC, int FA, int FB>
 hipError_t launch_tiles(const Fp8Args& P, hipStream_t s) {
   const int64_t n = (int64_t)P.tiles_m * P.tiles_n * P.splits;
-  if (n >= (1ll << 31) - 8) return hipErrorInvalidValue;
   const unsigned grid = (unsigned)((n + 7) / 8 * 8);
   constexpr int NT = 64 * WGM * WGN;
   if (P.c_f32) gemm_fp8_kernel<BM, BN, WGM, WGN, S, OCC, FA, FB, true><<<grid, NT, 0, s>>>(P);
   else gemm_fp8_kernel<BM, BN, WGM, WGN, S, OCC, FA, FB, false><<<grid, NT, 0, s>>>(P);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || P.splits == 1) return e;
-  const int64_t groups = P.M * cdiv(P.N, 4);
-  if (groups >= (1ll << 31) * 256ll) return hipErrorInvalidValue;
-  fp8_reduce_kernel<<<(unsigned)cdiv(groups, 256), 256, 0, s>>>(P);
+  fp8_reduce_kernel<<<element_blocks(P.M * cdiv(P.N, 4)), 256, 0, s>>>(P);
   return hipGetLastError();
 }
 
@@ -812,17 +813,17 @@ enum TileId { T256x256 = 0, T256x128, T128x128, T64x64, T_ROWS, kNumCfg };
 // (8192 x 2048 x 8192 104 us against 124).
 // [0]: bfloat16 results, [1]: float32.
 struct TileCfg {
-  int bm, bn, occ;
+  int bm, bn, threads, occ;
   struct {
     float lo, hi, fix, gbs;
   } t[2];
 };
 const TileCfg kCfgs[kNumCfg] = {
-    {256, 256, 1, {{0.98f, 0.69f, 15.0f, 1340.f}, {2.19f, 1.92f, 14.1f, 1920.f}}},  // 2 x 4 waves, 2 stages
-    {256, 128, 1, {{0.57f, 0.45f, 7.3f, 1320.f}, {1.19f, 1.11f, 8.0f, 1990.f}}},    // 4 x 2 waves, 3 stages
-    {128, 128, 2, {{0.42f, 0.57f, 5.0f, 1360.f}, {0.70f, 1.17f, 5.1f, 1980.f}}},    // 2 x 2 waves, 2 stages
-    {64, 64, 4, {{0.25f, 0.53f, 1.8f, 1200.f}, {0.35f, 0.92f, 2.0f, 2000.f}}},      // 2 x 2 waves, 2 stages
-    {32, 16, 1, {}},
+    {256, 256, 512, 1, {{0.98f, 0.69f, 15.0f, 1340.f}, {2.19f, 1.92f, 14.1f, 1920.f}}},  // 2 x 4 waves, 2 stages
+    {256, 128, 512, 1, {{0.57f, 0.45f, 7.3f, 1320.f}, {1.19f, 1.11f, 8.0f, 1990.f}}},    // 4 x 2 waves, 3 stages
+    {128, 128, 256, 2, {{0.42f, 0.57f, 5.0f, 1360.f}, {0.70f, 1.17f, 5.1f, 1980.f}}},    // 2 x 2 waves, 2 stages
+    {64, 64, 256, 4, {{0.25f, 0.53f, 1.8f, 1200.f}, {0.35f, 0.92f, 2.0f, 2000.f}}},      // 2 x 2 waves, 2 stages
+    {32, 16, 1024, 1, {}},
 };
 
 float estimate(int64_t M, int64_t N, int kb, bool f32, const TileCfg& c, int splits) {
@@ -855,17 +856,17 @@ hipError_t launch_cfg(const Fp8Args& P, int cfg, hipStream_t s) {
 
 // Columns of C without a product: the bias, or zero.
 __global__ __launch_bounds__(256) void fp8_bias_kernel(const Fp8Args P) {
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (idx >= P.M * P.N) return;
-  const int64_t m = idx / P.N, n = idx - m * P.N;
-  const float x = P.bias ? P.bias[n] : 0.f;
-  if (P.c_f32) ((float*)P.C)[m * P.ldc + n] = x;
-  else ((bf16_t*)P.C)[m * P.ldc + n] = f2bf(x);
+  for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < P.M * P.N; idx += (int64_t)gridDim.x * 256) {
+    const int64_t m = idx / P.N, n = idx - m * P.N;
+    const float x = P.bias ? P.bias[n] : 0.f;
+    if (P.c_f32) ((float*)P.C)[m * P.ldc + n] = x;
+    else ((bf16_t*)P.C)[m * P.ldc + n] = f2bf(x);
+  }
 }
 
 }  // namespace
 
-hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits, hipStream_t s) {
+hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits, hipStream_t s, int64_t max_threads) {
   Fp8Args P{};
   P.A = (const uint8_t*)d.A;
   P.B = (const uint8_t*)d.B;
@@ -893,19 +894,39 @@ hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits
   // parts the caches join (8192 x 2303 x 768 39 us, past them 47).
   P.past = P.M * P.N <= (48ll << 20) && P.ldc % 8 == 0 && ((uintptr_t)P.C & 15) == 0;
   if (P.kb == 0) {
-    if (P.M * P.N >= (1ll << 31) * 256ll) return hipErrorInvalidValue;
-    fp8_bias_kernel<<<(unsigned)cdiv(P.M * P.N, 256), 256, 0, s>>>(P);
+    fp8_bias_kernel<<<element_blocks(P.M * P.N), 256, 0, s>>>(P);
     return hipGetLastError();
   }
   if (cfg < 0 || cfg >= kNumCfg || (cfg == T_ROWS && (d.M > 32 || splits > 1))) return hipErrorInvalidValue;
   P.kb_split = (int32_t)(cdiv(cdiv(P.kb, std::max(1, splits)), 4) * 4);
   P.splits = (int32_t)cdiv(P.kb, P.kb_split);
   if (P.splits > 1 && (!d.workspace || d.workspace_bytes < (size_t)P.splits * P.M * P.N * 4)) return hipErrorInvalidValue;
-  P.tiles_m = (int32_t)cdiv(P.M, kCfgs[cfg].bm);
-  P.tiles_n = (int32_t)cdiv(P.N, kCfgs[cfg].bn);
   const bool a4 = d.a_dtype == LAYUP_E4M3, b4 = d.b_dtype == LAYUP_E4M3;
-  if (a4) return b4 ? launch_cfg<0, 0>(P, cfg, s) : launch_cfg<0, 1>(P, cfg, s);
-  return b4 ? launch_cfg<1, 0>(P, cfg, s) : launch_cfg<1, 1>(P, cfg, s);
+  // What one launch cannot take goes in slices of whole tiles, eight at least
+  // (scale blocks of 128 rows stay whole).  The slices' partial results follow
+  // one another through the same workspace.
+  const TileCfg& t = kCfgs[cfg];
+  auto slice = [](int64_t tiles, int64_t most) { return tiles <= most ? tiles : std::max<int64_t>(8, most / 8 * 8); };
+  const int64_t most = (max_threads / t.threads - 7) / P.splits;  // a launch's tiles go up to a multiple of 8
+  const int64_t rows = slice(cdiv(P.M, t.bm), most) * t.bm, cols = slice(cdiv(P.N, t.bn), most / (rows / t.bm)) * t.bn;
+  for (int64_t m = 0; m < d.M; m += rows)
+    for (int64_t n = 0; n < d.N; n += cols) {
+      Fp8Args Q = P;
+      Q.M = std::min(rows, d.M - m);
+      Q.N = std::min(cols, d.N - n);
+      Q.A += m * P.lda;
+      Q.B += n * P.ldb;
+      Q.sa += (m >> P.fa) * P.ldsa;
+      Q.sb += (n >> P.fb) * P.ldsb;
+      Q.C = (char*)P.C + (m * P.ldc + n) * (P.c_f32 ? 4 : 2);
+      if (P.bias) Q.bias += n;
+      Q.tiles_m = (int32_t)cdiv(Q.M, t.bm);
+      Q.tiles_n = (int32_t)cdiv(Q.N, t.bn);
+      const hipError_t e = a4 ? (b4 ? launch_cfg<0, 0>(Q, cfg, s) : launch_cfg<0, 1>(Q, cfg, s))
+                              : (b4 ? launch_cfg<1, 0>(Q, cfg, s) : launch_cfg<1, 1>(Q, cfg, s));
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
 }
 
 hipError_t launch_gemm_fp8(const layup_gemm_fp8_desc& d, hipStream_t s) {

@@ -291,7 +291,8 @@ int64_t norm_partial_rows(int64_t rows, int d);
 int64_t norm_partial_floats(int64_t rows, int d);
 hipError_t launch_quant_fp8(const layup_quant_desc& d, hipStream_t s);
 hipError_t launch_gemm_fp8(const layup_gemm_fp8_desc& d, hipStream_t s);
-hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits, hipStream_t s);
+hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits, hipStream_t s,
+                               int64_t max_threads = MAX_LAUNCH_THREADS);
 
 // Records the text of a context-free call's error; returns st.  (model.hip)
 layup_status global_fail(layup_status st, const std::string& msg);
@@ -313,4 +314,6 @@ int layup_test_gemm_tile(const layup_gemm_desc* d, int32_t n, int32_t group, int
                          int64_t run, const layup_tensor* upd, const layup_hparams* hp, float alpha, void* stream);
 // An 8-bit product with the tile configuration and split of K given; cfg < 0: the plan the library chooses.
 int layup_test_gemm_fp8_tile(const layup_gemm_fp8_desc* d, int32_t cfg, int32_t splits, void* stream);
+// The same with the threads that a launch may have.
+int layup_test_gemm_fp8_slices(const layup_gemm_fp8_desc* d, int32_t cfg, int32_t splits, int64_t max_threads, void* stream);
 }

@@ -187,7 +187,8 @@ layup_status layup_quant_fp8(const layup_quant_desc* d, void* stream) {
   });
 }
 
-static layup_status gemm_fp8(const layup_gemm_fp8_desc* d, int cfg, int splits, void* stream) {
+static layup_status gemm_fp8(const layup_gemm_fp8_desc* d, int cfg, int splits, void* stream,
+                             int64_t max_threads = MAX_LAUNCH_THREADS) {
   return call(d, stream, "8-bit product", [&](hipStream_t s) {
     const int64_t top = 1ll << 31;
     need(d->M >= 0 && d->N >= 0 && d->K >= 0 && d->M < top && d->N < top && d->K < top, LAYUP_ERR_SHAPE,
@@ -208,7 +209,7 @@ static layup_status gemm_fp8(const layup_gemm_fp8_desc* d, int cfg, int splits, 
            "leading dimensions above 2^24 are not supported");
     }
     need(aligned(d->workspace, 16), LAYUP_ERR_ALIGN, "workspace must be 16-byte aligned");
-    return cfg < 0 ? launch_gemm_fp8(*d, s) : launch_gemm_fp8_cfg(*d, cfg, splits, s);
+    return cfg < 0 ? launch_gemm_fp8(*d, s) : launch_gemm_fp8_cfg(*d, cfg, splits, s, max_threads);
   });
 }
 
@@ -216,6 +217,10 @@ layup_status layup_gemm_fp8(const layup_gemm_fp8_desc* d, void* stream) { return
 
 int layup_test_gemm_fp8_tile(const layup_gemm_fp8_desc* d, int32_t cfg, int32_t splits, void* stream) {
   return gemm_fp8(d, cfg, splits, stream);
+}
+
+int layup_test_gemm_fp8_slices(const layup_gemm_fp8_desc* d, int32_t cfg, int32_t splits, int64_t max_threads, void* stream) {
+  return gemm_fp8(d, cfg, splits, stream, max_threads);
 }
 
 }  // extern "C"
