@@ -485,6 +485,9 @@ def _call(f, desc, stream):
 def _mask(p, seed, offset, offset_dev) -> layup_dropout_mask:
     if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
         raise ValueError("seed and offset are unsigned 64-bit numbers")
+    if offset_dev is not None and not isinstance(offset_dev, int):
+        if str(offset_dev.dtype) not in ("torch.int64", "torch.uint64") or offset_dev.numel() < 1:
+            raise ValueError("offset_dev is a 64-bit integer on the device")
     return layup_dropout_mask(p=p, seed=seed, offset=offset, offset_dev=_ptr(offset_dev))
 
 

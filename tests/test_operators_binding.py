@@ -1,0 +1,19 @@
+"""What the descriptors of the dropout, LayerNorm and 8-bit calls take from tensors and refuse.  No GPU needed."""
+import pytest
+
+from paper_2410_05985_amd import layup as LU
+
+torch = pytest.importorskip("torch")
+
+
+def test_offset_from_the_device_is_a_64_bit_integer():
+    """The kernels read eight bytes there."""
+    x = torch.zeros(4, 8)
+    for t in (torch.int64, torch.uint64):
+        assert LU.dropout_desc(x, x, p=0.5, offset_dev=torch.zeros(1, dtype=t)).drop.offset_dev
+    assert LU.dropout_desc(x, x, p=0.5, offset_dev=0x1000).drop.offset_dev == 0x1000
+    for bad in (torch.zeros(1, dtype=torch.int32), torch.zeros(1), torch.zeros(0, dtype=torch.int64)):
+        with pytest.raises(ValueError):
+            LU.dropout_desc(x, x, p=0.5, offset_dev=bad)
+        with pytest.raises(ValueError):
+            LU.layernorm_desc(x, x, p=0.5, offset_dev=bad)
