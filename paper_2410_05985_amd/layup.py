@@ -459,6 +459,15 @@ def _vector(t, n: int, kind: str):
     return t.data_ptr()
 
 
+def _workspace(t):
+    """(address, bytes) of a workspace tensor of any type."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("a workspace of adjacent elements is needed")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _same_type(*ts):
     codes = {_dtype(t) for t in ts if t is not None}
     if len(codes) > 1:
@@ -554,8 +563,7 @@ def layernorm_grad_desc(dy, s, mean, rstd, gamma=None, dsum=None, dres=None, dx=
     d.dx_dtype = d.dy_dtype if dx is None else _dtype(dx)
     d.gamma, d.dgamma, d.dbeta = (_vector(v, d.d, "torch.float32") for v in (gamma, dgamma, dbeta))
     d.mean, d.rstd = (_vector(v, d.rows, "torch.float32") for v in (mean, rstd))
-    if workspace is not None:
-        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    d.workspace, d.workspace_bytes = _workspace(workspace)
     d.drop = _mask(p, seed, offset, offset_dev)
     return _keep(d, dy, s, mean, rstd, gamma, dsum, dres, dx, dgamma, dbeta, workspace, offset_dev)
 
@@ -613,8 +621,7 @@ def gemm_fp8_desc(A, a_scale, a_block: int, B, b_scale, b_block: int, C_, K: int
     d.b_scale, d.ld_b_scale = _scale(b_scale, -(-d.N // max(1, b_block)), K)
     d.a_dtype, d.b_dtype, d.a_block, d.b_block = _dtype(A), _dtype(B), a_block, b_block
     d.bias = _vector(bias, d.N, "torch.float32")
-    if workspace is not None:
-        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    d.workspace, d.workspace_bytes = _workspace(workspace)
     return _keep(d, A, a_scale, B, b_scale, C_, bias, workspace)
 
 

@@ -17,3 +17,19 @@ def test_offset_from_the_device_is_a_64_bit_integer():
             LU.dropout_desc(x, x, p=0.5, offset_dev=bad)
         with pytest.raises(ValueError):
             LU.layernorm_desc(x, x, p=0.5, offset_dev=bad)
+
+
+def test_workspace_is_one_piece_of_memory():
+    """Its bytes are counted from its elements: an expanded or strided one holds fewer, or others' between them."""
+    x, v = torch.zeros(4, 8), torch.zeros(4)
+    q = torch.zeros(4, 128, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    e = torch.zeros(4, 4, dtype=torch.uint8)
+    room = torch.zeros(4096, dtype=torch.uint8)
+    assert LU.layernorm_grad_desc(x, x, v, v, workspace=room).workspace_bytes == 4096
+    assert LU.gemm_fp8_desc(q, e, 1, q, e, 1, torch.zeros(4, 4), 128, workspace=room).workspace_bytes == 4096
+    assert not LU.layernorm_grad_desc(x, x, v, v).workspace
+    for bad in (room[::2], torch.zeros(1).expand(1 << 20)):
+        with pytest.raises(ValueError):
+            LU.layernorm_grad_desc(x, x, v, v, workspace=bad)
+        with pytest.raises(ValueError):
+            LU.gemm_fp8_desc(q, e, 1, q, e, 1, torch.zeros(4, 4), 128, workspace=bad)
