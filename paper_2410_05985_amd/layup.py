@@ -481,13 +481,23 @@ def _keep(d, *tensors):
     devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
     if len(devices) > 1:
         raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
-    d.in_host_memory = any(x.type == "cpu" for x in devices)
+    d.device = devices.pop() if devices else None
     return d
 
 
 def _call(f, desc, stream):
-    if getattr(desc, "in_host_memory", False):
+    """The call on a stream of the tensors' device; without one, on that device's default stream."""
+    dev = getattr(desc, "device", None)
+    if dev is not None and dev.type == "cpu":
         raise ValueError("tensors in host memory")
+    if dev is not None and not isinstance(stream, int):
+        if stream is None:
+            import torch
+            if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+                with torch.cuda.device(dev):
+                    return _check(f(C.byref(desc), None))
+        elif stream.device != dev:
+            raise ValueError(f"a stream of {stream.device} for tensors on {dev}")
     _check(f(C.byref(desc), _stream(stream)))
 
 

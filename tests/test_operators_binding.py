@@ -33,3 +33,48 @@ def test_workspace_is_one_piece_of_memory():
             LU.layernorm_grad_desc(x, x, v, v, workspace=bad)
         with pytest.raises(ValueError):
             LU.gemm_fp8_desc(q, e, 1, q, e, 1, torch.zeros(4, 4), 128, workspace=bad)
+
+
+class Stream:
+    cuda_stream = 0x1234
+
+    def __init__(self, device):
+        self.device = torch.device(device)
+
+
+def descriptor_on(device):
+    d = LU.layup_dropout_desc()
+    d.device = torch.device(device)
+    return d
+
+
+def test_a_stream_of_another_device_is_refused():
+    calls = []
+    f = lambda d, s: calls.append(s) or LU.LAYUP_OK  # noqa: E731
+    with pytest.raises(ValueError):
+        LU._call(f, descriptor_on("cuda:1"), Stream("cuda:0"))
+    assert not calls
+    LU._call(f, descriptor_on("cuda:1"), Stream("cuda:1"))
+    LU._call(f, descriptor_on("cuda:1"), 0x5678)  # a bare hipStream_t is the caller's word
+    assert calls == [0x1234, 0x5678]
+
+
+def test_no_stream_is_the_default_stream_of_the_tensors_device(monkeypatch):
+    """NULL is the current device's default stream: that device has to be the tensors' during the call."""
+    current, seen = [0], []
+
+    class Device:
+        def __init__(self, d):
+            self.d = d.index
+
+        def __enter__(self):
+            self.old, current[0] = current[0], self.d
+
+        def __exit__(self, *_):
+            current[0] = self.old
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for dev in ("cuda:1", "cuda:0"):
+        LU._call(lambda d, s: seen.append((s, current[0])) or LU.LAYUP_OK, descriptor_on(dev), None)
+    assert seen == [(None, 1), (None, 0)] and current == [0]
