@@ -96,6 +96,20 @@ def quantise(x, fmt, block_rows):
     return q, (e + 127).astype(np.uint8)
 
 
+def quantise_all(x, fmt, block_rows):
+    """quantise, all blocks at once: amax = m 2^e with 1/2 <= m < 1 has the exponent e - 1 - top, one more above 7/8."""
+    x = np.asarray(x, np.float64)
+    rows, cols = x.shape
+    nr, nc = -(-rows // block_rows), -(-cols // 128)
+    fin = np.isfinite(x)
+    t = np.zeros((nr * block_rows, nc * 128))
+    t[:rows, :cols] = np.abs(np.where(fin, x, 0.0))
+    m, e = np.frexp(t.reshape(nr, block_rows, nc, 128).max((1, 3)))
+    e = np.where(m > 0, np.maximum(e - 1 - TOPS[fmt][0] + (m > 0.875), -126), 0).astype(np.int64)
+    each = np.repeat(np.repeat(e, block_rows, 0)[:rows], 128, 1)[:, :cols]
+    return np.where(fin, round_fp8(np.ldexp(np.where(fin, x, 0.0), -each), fmt), np.nan), (e + 127).astype(np.uint8)
+
+
 def value(q, scale, block_rows):
     """The values that 8-bit values and scale bytes stand for."""
     rows, cols = q.shape
