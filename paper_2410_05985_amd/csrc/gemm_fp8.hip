@@ -6,17 +6,23 @@
 // The 8-bit matrix instructions align eight products at a time and drop what
 // lies 2^-13 below the largest (measured: a product of 2^(16-g) beside one of
 // 2^16 is kept up to g = 13 within a group of eight, up to g = 23 outside it;
-// the scaled and the plain instruction give the same bits).  A result is off
-// by 1.3e-5 of itself for normal operands whatever K: nothing next to the
-// rounding of a bfloat16 result (1.7e-3), but fifty times a float32 sum's
-// error.  So a float32 result (EXACT) is computed from the operands widened in
-// registers to bfloat16, which holds them exactly, scale included, at the
-// bfloat16 instructions' half rate.  Its range ends before the least values
-// times the least scales and the largest times the largest: a wave that meets
-// such a scale byte computes its results again from the values alone
-// (plain_sum; 4096 x 1024 x 8192 with one in every row 6.7 ms, else 66 us.
-// Watching for them costs up to 4 %: 1 x 2048 x 8192 7.4 -> 7.7 us, 2048 x 2048 x
-// 2048 21.7 -> 22.5, 4000 x 4000 x 16384 398 -> 402).
+// the scaled and the plain instruction give the same bits).  For operands of
+// random signs a sum is off by 1.2e-5 to 1.5e-5 of the results' size whatever K
+// (2e-5 to 3e-5 where some k are much louder), for positive ones by 1.5e-6 to
+// 2.9e-6, always too small; never by more than 1.7e-5 of the products' added
+// magnitudes.  That changes one or two in a hundred bfloat16 results, by a step
+// of theirs, and leaves their distance from the exact product at that of the
+// rounding, 1.66e-3; but it is fifty times a float32 sum's error, and where a sum
+// cancels not small next to the result.
+//
+// So a float32 result (EXACT) is computed from the operands widened in registers
+// to bfloat16, which holds them exactly, scale included, at the bfloat16
+// instructions' half rate.  Its range ends before the least values times the
+// least scales and the largest times the largest: a wave that meets such a scale
+// byte computes its results again from the values alone (plain_sum; 4096 x 1024 x
+// 8192 with one in every row 6.7 ms, else 66 us.  Watching for them costs up to
+// 4 %: 1 x 2048 x 8192 7.4 -> 7.7 us, 2048 x 2048 x 2048 21.7 -> 22.5, 4000 x
+// 4000 x 16384 398 -> 402).
 #include "lds_pipe.h"
 
 namespace layup {

@@ -11,7 +11,7 @@ from oracle import operators_ref as R
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 from paper_2410_05985_amd import layup as LU  # noqa: E402
-from tests.test_gpu_operators import BF16, DEV, EPS, F32, FP8, TILES, U, f64, near, product_bound, tile_call, values  # noqa: E402
+from tests.test_gpu_operators import BF16, DEV, EPS, F32, FP8, TILES, U, f64, near, product_bound, quantised, tile_call, values  # noqa: E402
 
 
 def operand(rng, rows, K, fmt, first, last):
@@ -109,3 +109,26 @@ def test_quantiser_then_product_of_tiny_and_huge_blocks(M, size, fmt):
     torch.cuda.synchronize()
     va, vb = values(qa, ea, K, 1), values(qb, eb, K, 1)
     near(f64(c), va @ vb.T, product_bound(va, vb, F32) + U * np.abs(va @ vb.T), "product")
+
+
+@pytest.mark.parametrize("M", [3, 70, 300])
+@pytest.mark.parametrize("K", [384, 4500])
+@pytest.mark.parametrize("signs", [True, False])
+@pytest.mark.parametrize("out", [F32, BF16])
+def test_sums_that_cancel(M, K, signs, out):
+    """The bias takes the product away, so that the result is the sum's error alone: within the bound of the matrix
+    unit's sums for a bfloat16 C, of float32 sums for a float32 C."""
+    rng = np.random.default_rng(K)
+    N = 130
+    row, b = rng.normal(size=(1, K)), rng.normal(size=(N, K))
+    if not signs:
+        row, b = np.abs(row), np.abs(b)
+    (qa, ea), (qb, eb) = (quantised(torch.from_numpy(x).float().to(DEV), 1, "e4m3") for x in (np.repeat(row, M, 0), b))
+    va, vb = values(qa, ea, K, 1), values(qb, eb, K, 1)
+    bias = torch.from_numpy(-(vb @ va[0])).float().to(DEV)
+    c = torch.empty(M, N, dtype=out, device=DEV)
+    LU.layup_gemm_fp8(LU.gemm_fp8_desc(qa, ea, 1, qb, eb, 1, c, K, bias=bias), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    ref = va @ vb.T + f64(bias)
+    tol = product_bound(va, vb, out) + U * (np.abs(ref) + np.abs(f64(bias)))
+    near(f64(c), ref, tol + EPS[out] * (np.abs(ref) + tol), "product")
