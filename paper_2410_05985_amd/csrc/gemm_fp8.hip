@@ -41,7 +41,6 @@ struct Fp8Args {
   int32_t kb;      // K in blocks of 128
   int32_t c_f32, splits, kb_split;  // blocks of a split: a multiple of 4
   int32_t tiles_m, tiles_n;
-  int32_t past;  // bfloat16 results around the caches
 };
 
 // Eight 8-bit values, times a power of two, in bfloat16: exact.
@@ -537,6 +536,13 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
   // rows' 64-byte pieces.  The pieces carry the alignment of one element (element
   // by element 8192 x 2303 x 768 took 66 us, now 39; 2304 columns 24); what the
   // last column cuts goes by the element.
+  //
+  // Stores around the caches are not used: alone the product mostly gains (4096 x
+  // 14592 x 512 67 -> 59 us, 8192 x 8512 x 1536 140 -> 123), but whoever reads the
+  // result next pays more (with a quantiser behind it 102 -> 112 and 182 -> 183; 40
+  // to 256 MB of results at three K: up to 16 % lost, at most 3 % won).  Up to 20 MB
+  // of whole 64-byte pieces product and reader win 1 % on average, and off those
+  // lose up to 19 % (8192 x 1000 x 600 20.8 -> 24.7).
   const bool part = P.splits > 1;
   const bool wide = part || EXACT;  // float32 stores
   float* const cf = part ? P.partial + (int64_t)split * P.M * P.N : (float*)P.C;
@@ -611,15 +617,7 @@ __device__ __forceinline__ void tile_item(const Fp8Args& P, int lid) {
         if (n + 8 <= P.N) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            if (mb + 16 * y + l4 >= P.M) continue;
-            const V v = u32x4{w[y][0], w[y][1], w[y][2], w[y][3]};
-            if (P.past) {
-              asm volatile("");  // or the two stores become one, without the hint
-              __builtin_nontemporal_store(v, reinterpret_cast<V*>(to[y]));
-              asm volatile("");
-            } else {
-              *reinterpret_cast<V*>(to[y]) = v;
-            }
+            if (mb + 16 * y + l4 < P.M) *reinterpret_cast<V*>(to[y]) = u32x4{w[y][0], w[y][1], w[y][2], w[y][3]};
           }
         } else if (n < P.N) {
 #pragma unroll
@@ -892,13 +890,6 @@ hipError_t launch_gemm_fp8_cfg(const layup_gemm_fp8_desc& d, int cfg, int splits
   P.fb = d.b_block == 128 ? 7 : 0;
   P.kb = (int32_t)cdiv(d.K, 128);
   P.c_f32 = d.c_f32 != 0;
-  // Around the caches a result leaves them to the operands (8192 x 2304 x 768
-  // behind its LayerNorm 43.7 us, else 49.1; 8192 x 4096 x 1024 with a reader of
-  // the result 68, else 74).  From 96 MB on the product gains nothing and its
-  // reader loses (8192 x 8192 x 2048, 134 MB, with a reader 212 us, else 186).
-  // Rows that do not start on 16 bytes share lines with their neighbours, whose
-  // parts the caches join (8192 x 2303 x 768 39 us, past them 47).
-  P.past = P.M * P.N <= (48ll << 20) && P.ldc % 8 == 0 && ((uintptr_t)P.C & 15) == 0;
   if (P.kb == 0) {
     fp8_bias_kernel<<<element_blocks(P.M * P.N), 256, 0, s>>>(P);
     return hipGetLastError();
