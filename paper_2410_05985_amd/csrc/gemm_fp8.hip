@@ -808,13 +808,11 @@ enum TileId { T256x256 = 0, T256x128, T128x128, T64x64, T_ROWS, kNumCfg };
 // Estimate of a product's time.  occ workgroups share a CU; a step of 128 k
 // takes lo us alone on a CU and hi with the CU full (occ = 1: on an empty and
 // on a full chip), a tile fix us besides (first copies, stores), a byte of C
-// 1 / gbs ns.  Fitted to 1008 timings of 70 products of 65 to 8192 a side, with
-// operands and result in rotation: the choice takes 1.01 of the best tile and
-// split's time on average, 1.25 at most.  The figures rank; they are no forecast
-// (a tile's fix holds what the loop cannot overlap).  One is not the fit's: a
-// 256 x 256 tile's 13.0 for bfloat16 is raised to 15, since the fit took it for
-// 8192 x 4096 x 1024 (47 us, on 128 x 128 42); it stays the choice at a longer K
-// (8192 x 2048 x 8192 104 us against 124).
+// 1 / gbs ns.  Fitted to 9600 timings of 700 products of 64 to 8192 a side, drawn
+// at random, with operands and result in rotation (off by 7 to 12 % of a time);
+// on 130 products not among them the choice takes 1.008 of the best tile and
+// split's time on average, 1.12 at most (among the 700 1.25), bfloat16 and float32
+// results alike.
 // [0]: bfloat16 results, [1]: float32.
 struct TileCfg {
   int bm, bn, threads, occ;
@@ -823,10 +821,10 @@ struct TileCfg {
   } t[2];
 };
 const TileCfg kCfgs[kNumCfg] = {
-    {256, 256, 512, 1, {{0.98f, 0.69f, 15.0f, 1340.f}, {2.19f, 1.92f, 14.1f, 1920.f}}},  // 2 x 4 waves, 2 stages
-    {256, 128, 512, 1, {{0.57f, 0.45f, 7.3f, 1320.f}, {1.19f, 1.11f, 8.0f, 1990.f}}},    // 4 x 2 waves, 3 stages
-    {128, 128, 256, 2, {{0.42f, 0.57f, 5.0f, 1360.f}, {0.70f, 1.17f, 5.1f, 1980.f}}},    // 2 x 2 waves, 2 stages
-    {64, 64, 256, 4, {{0.25f, 0.53f, 1.8f, 1200.f}, {0.35f, 0.92f, 2.0f, 2000.f}}},      // 2 x 2 waves, 2 stages
+    {256, 256, 512, 1, {{1.07f, 1.18f, 5.4f, 4420.f}, {2.26f, 2.50f, 6.5f, 5370.f}}},  // 2 x 4 waves, 2 stages
+    {256, 128, 512, 1, {{0.61f, 0.68f, 3.5f, 4450.f}, {1.30f, 1.40f, 4.2f, 5870.f}}},  // 4 x 2 waves, 3 stages
+    {128, 128, 256, 2, {{0.47f, 0.74f, 2.6f, 4560.f}, {0.80f, 1.33f, 3.1f, 5700.f}}},  // 2 x 2 waves, 2 stages
+    {64, 64, 256, 4, {{0.28f, 0.57f, 1.3f, 3710.f}, {0.39f, 0.95f, 1.8f, 5950.f}}},    // 2 x 2 waves, 2 stages
     {32, 16, 1024, 1, {}},
 };
 
