@@ -481,23 +481,24 @@ def _keep(d, *tensors):
     devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
     if len(devices) > 1:
         raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
-    d.device = devices.pop() if devices else None
+    dev = devices.pop() if devices else None
+    d.on = None if dev is None else -1 if dev.type == "cpu" else dev.index  # index of the GPU, -1: the host
     return d
 
 
 def _call(f, desc, stream):
     """The call on a stream of the tensors' device; without one, on that device's default stream."""
-    dev = getattr(desc, "device", None)
-    if dev is not None and dev.type == "cpu":
-        raise ValueError("tensors in host memory")
-    if dev is not None and not isinstance(stream, int):
+    on = getattr(desc, "on", None)
+    if on is not None:
+        if on < 0:
+            raise ValueError("tensors in host memory")
         if stream is None:
             import torch
-            if dev.type == "cuda" and dev.index != torch.cuda.current_device():
-                with torch.cuda.device(dev):
+            if on != torch.cuda.current_device():
+                with torch.cuda.device(on):
                     return _check(f(C.byref(desc), None))
-        elif stream.device != dev:
-            raise ValueError(f"a stream of {stream.device} for tensors on {dev}")
+        elif not isinstance(stream, int) and stream.device_index != on:
+            raise ValueError(f"a stream of device {stream.device_index} for tensors on device {on}")
     _check(f(C.byref(desc), _stream(stream)))
 
 

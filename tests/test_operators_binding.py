@@ -39,23 +39,27 @@ class Stream:
     cuda_stream = 0x1234
 
     def __init__(self, device):
-        self.device = torch.device(device)
+        self.device_index = device
 
 
 def descriptor_on(device):
-    d = LU.layup_dropout_desc()
-    d.device = torch.device(device)
-    return d
+    """A descriptor as of tensors on that GPU."""
+    return LU._keep(LU.layup_dropout_desc(), Tensor(device))
+
+
+class Tensor:
+    def __init__(self, device):
+        self.device = torch.device("cuda", device)
 
 
 def test_a_stream_of_another_device_is_refused():
     calls = []
     f = lambda d, s: calls.append(s) or LU.LAYUP_OK  # noqa: E731
     with pytest.raises(ValueError):
-        LU._call(f, descriptor_on("cuda:1"), Stream("cuda:0"))
+        LU._call(f, descriptor_on(1), Stream(0))
     assert not calls
-    LU._call(f, descriptor_on("cuda:1"), Stream("cuda:1"))
-    LU._call(f, descriptor_on("cuda:1"), 0x5678)  # a bare hipStream_t is the caller's word
+    LU._call(f, descriptor_on(1), Stream(1))
+    LU._call(f, descriptor_on(1), 0x5678)  # a bare hipStream_t is the caller's word
     assert calls == [0x1234, 0x5678]
 
 
@@ -65,7 +69,7 @@ def test_no_stream_is_the_default_stream_of_the_tensors_device(monkeypatch):
 
     class Device:
         def __init__(self, d):
-            self.d = d.index
+            self.d = d
 
         def __enter__(self):
             self.old, current[0] = current[0], self.d
@@ -75,6 +79,6 @@ def test_no_stream_is_the_default_stream_of_the_tensors_device(monkeypatch):
 
     monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
     monkeypatch.setattr(torch.cuda, "device", Device)
-    for dev in ("cuda:1", "cuda:0"):
+    for dev in (1, 0):
         LU._call(lambda d, s: seen.append((s, current[0])) or LU.LAYUP_OK, descriptor_on(dev), None)
     assert seen == [(None, 1), (None, 0)] and current == [0]
