@@ -197,6 +197,10 @@ layup_status layup_refresh_shadow(layup_ctx* ctx);
  * completed steps and site is 0 for the embeddings, 1 + 2l and 2 + 2l for
  * block l's attention and MLP: a step repeated from the same state draws the
  * same masks.  A backward draws its forward's masks, whatever was set since.
+ * Masks depend on nothing else, so give a seed of its own to each of several
+ * contexts (replicas), to a new context that takes up a run (its steps count from
+ * 0 again), and to each step where unit 0 is updated by other calls than the
+ * context's (the count then stands still).
  * p = 0 (the initial state) turns dropout off.  0 <= p < 1; LAYUP_ERR_DTYPE for
  * the MLP. */
 layup_status layup_set_dropout(layup_ctx* ctx, float p, uint64_t seed);

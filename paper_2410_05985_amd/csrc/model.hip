@@ -466,6 +466,11 @@ hipError_t residual_norm(layup_ctx* c, float* branch, const float* residual, int
   return launch_norm_fwd(n, site_mask(c, site), c->sc);
 }
 
+// Without dropout the products' epilogues add the residual and the LayerNorm reads
+// its sum alone (launch_layernorm_fwd): of 8192 x 768 8.5 us inside the step, with
+// the branch, the residual and their sum here 16.6.  Backward 26.5 and 30.2.  The
+// step without dropout so keeps its bits too.
+//
 // Backward of a LayerNorm: dx (float32) = dres + the LayerNorm's part, dy16
 // (nullable) its bfloat16 copy, dropped as the branch of `site` was; partial
 // rows of the weights' gradients in part.

@@ -25,6 +25,9 @@ struct BwdArgs {
 // residual stream 22 us (4.6 TB/s) and the sums 4.  The next row's loads before
 // this row's sums were measured: 1237 columns 41.3 -> 37.7 us, 8192 columns 141
 // -> 140, a float32 stream of 2048 columns 55 -> 56, 768 columns 22 -> 24; not kept.
+// Above 8192 columns 1024 threads leave a thread 128 registers, and 20 to 47 of
+// what it keeps between rows are spilled: 4096 x 12288 bfloat16 103 us without the
+// sums (4.9 TB/s), 130 with them, whose partial rows are 50 MB.
 // WHOLE: d is a multiple of 8.
 template <class TY, class TS, class TX, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(const BwdArgs P) {
